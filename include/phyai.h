@@ -351,6 +351,145 @@ int phyai_profile_stage(phyai_expert* e, int32_t stage, int32_t reps, void* stre
  * "Quantization").  Codes 0x7f/0xff (NaN) give a NaN pattern. */
 int phyai_fp8_to_bf16(const uint8_t* codes, uint16_t* out, int64_t n, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The paged key/value cache.
+ *
+ * A language part that is fed in chunks (image tokens first, text as it
+ * arrives, then token by token) keeps each request's keys and values in pages
+ * of a pool that all requests share.  Per layer and chunk: phyai_qk_norm_rope
+ * (norms and rotation of queries and keys), phyai_paged_append (new keys and
+ * values into the pages), phyai_paged_attention (the new tokens over everything
+ * the request has in the cache); phyai_paged_gather copies the pages into the
+ * contiguous prefix that phyai_denoise reads.
+ *
+ * Batches are padded: request b has new_len[b] valid rows of `rows`; rows
+ * behind them are neither read nor written.  Lengths and page tables are
+ * device memory, so that a captured call serves every later length; the host
+ * checks what bounds them, and a kernel that meets a value outside those bounds
+ * does not follow it: it raises a bit in *status (device int32, or NULL) and
+ * treats the request as stated at each entry point.
+ *   PHYAI_PAGED_BAD_PAGE    a page number outside 0 .. n_pages-1
+ *   PHYAI_PAGED_BAD_LENGTH  a length outside what the call allows
+ * Bits are only ever set; the caller clears the word.
+ *
+ * These calls keep nothing, allocate nothing and may be captured into a graph.
+ * Calls on several streams may overlap where their outputs and workspaces do
+ * not. */
+#define PHYAI_PAGED_BAD_PAGE 1
+#define PHYAI_PAGED_BAD_LENGTH 2
+
+/* The pools and the table of a batch.  Token p of request b is row p % page_size
+ * of page page_table[b * table_stride + p / page_size].  A layer's pools lie
+ * layer_stride behind the layer before; inside, page, token and head strides are
+ * free (so pages may be ordered token-major or head-major), the same for keys and
+ * values, in elements, multiples of 16 bytes; a head's values are contiguous.
+ * Entries of the table behind a request's last page are never followed. */
+typedef struct {
+  void* k;                  /* device, 16-byte aligned                                            */
+  void* v;
+  const float* k_scale;     /* FP8E4M3: device [n_kv_heads] >= 0, value = code * scale; else NULL  */
+  const float* v_scale;
+  const int32_t* page_table;/* device                                                             */
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+  int32_t dtype;            /* F32, BF16 or FP8E4M3                                               */
+  int32_t n_layers, n_kv_heads;
+  int32_t head_dim;         /* 64, 128 or 256                                                     */
+  int32_t page_size;        /* tokens; a power of two, 16 .. 4096                                 */
+  int32_t n_pages;          /* pages of a pool                                                    */
+  int32_t batch;            /* requests of the table                                              */
+  int32_t max_pages;        /* entries of the table per request                                   */
+  int32_t table_stride;     /* >= max_pages                                                       */
+} phyai_paged_cache;
+
+/* The rows of one kind of head: value i of head h of token t of request b is at
+ * data[b * batch_stride + t * token_stride + h * head_stride + i].  Strides are
+ * >= 0 and multiples of 16 bytes, data is 16-byte aligned: queries, keys and
+ * values side by side in one projected row need no copy. */
+typedef struct {
+  void* data;               /* device                                                             */
+  int64_t batch_stride, token_stride, head_stride;   /* elements                                  */
+  int32_t n_heads;
+} phyai_head_rows;
+
+/* Norms of queries and keys for each head and their rotation, in one pass:
+ * y = x / sqrt(mean(x^2) + eps) * (1 + gain), then pairs (i, i + head_dim/2)
+ * rotated by position * rope_base^(-2i/head_dim).  Row t of request b stands at
+ * position past_len[b] + t.
+ *
+ *   q, k          inputs; either may be NULL.  q_out, k_out: outputs of the same
+ *                 head counts; the same rows as the input (in place) or rows that
+ *                 do not overlap it.
+ *   q_gain, k_gain  device float32 [head_dim], 16-byte aligned, or NULL (gain 0).
+ *   eps           > 0: normalise; 0: rotate only (gains must be NULL).
+ *   rope_base     >= 1: rotate; 0: normalise only.
+ *   past_len      device [batch], or NULL (0).   new_len  device [batch], or NULL (rows).
+ *   dtype         F32 or BF16 of every row.  Sums, norms and angles are held in 32
+ *                 bits or more (angles exact to 2^-31 of a turn at any position).
+ *
+ * A request whose lengths are out of range (new_len outside 0..rows, past_len < 0) is
+ * not touched (PHYAI_PAGED_BAD_LENGTH). */
+int phyai_qk_norm_rope(const phyai_head_rows* q, const phyai_head_rows* k, const phyai_head_rows* q_out,
+                       const phyai_head_rows* k_out, const float* q_gain, const float* k_gain, float eps,
+                       float rope_base, const int32_t* past_len, const int32_t* new_len, int32_t batch,
+                       int32_t rows, int32_t head_dim, int32_t dtype, int32_t* status, void* stream);
+
+/* Append the keys and values of new tokens to the pages of a layer: row t of
+ * request b goes to token past_len[b] + t, the key rotated to that position on the
+ * way (rope_base >= 1; 0: stored as it is).  The cache of dtype F32 takes F32
+ * rows, BF16 and FP8E4M3 take BF16 rows; 8-bit codes are value / scale to the
+ * nearest, ties to even, saturated at 448.
+ *
+ * Not written: requests with past_len + new_len beyond max_pages * page_size or a
+ * length out of range (PHYAI_PAGED_BAD_LENGTH), tokens whose page number is out of
+ * range (PHYAI_PAGED_BAD_PAGE).  Requests that share a page to be written race. */
+int phyai_paged_append(const phyai_paged_cache* cache, int32_t layer, const phyai_head_rows* k,
+                       const phyai_head_rows* v, float rope_base, const int32_t* past_len, const int32_t* new_len,
+                       int32_t rows, int32_t dtype, int32_t* status, void* stream);
+
+/* Attention of the last new_len[b] tokens of a request over its kv_len[b] tokens in
+ * the cache (its own keys among them, appended before): o = sum_j p_j v_j with
+ * p = softmax(scale * q . k_j) over the keys that a row sees.  Row t stands at
+ * position kv_len - new_len + t.  causal = 0: it sees every key; 1: those at
+ * positions up to its own; window > 0 (causal only): the last `window` of these.
+ * A row that sees no key is zero.  What lies in hidden rows of the cache, NaN and
+ * infinities included, does not reach the result.
+ *
+ *   q, out        rows of dtype F32 (cache F32) or BF16 (cache BF16 or FP8E4M3);
+ *                 query head h reads K/V head h / (n_heads / n_kv_heads).  `out`
+ *                 must not overlap `q` or the cache.
+ *   kv_len        device [batch], 0 .. max_kv_len.   new_len: device, or NULL (rows).
+ *   max_kv_len    host: the longest kv_len of this call (and of every replay of a
+ *                 captured one), 1 .. max_pages * page_size.  It decides how the
+ *                 keys are split, so results may differ in the last bits with it.
+ *   scale         > 0 and finite.
+ *   workspace     device, 16-byte aligned, at least phyai_paged_attention_workspace()
+ *                 bytes, not shared with a call that may overlap; may be NULL when
+ *                 that is 0.  Nothing in it is kept from call to call.
+ *
+ * A request with a length out of range gets NaN rows (PHYAI_PAGED_BAD_LENGTH;
+ * new_len below 0: none, above rows: `rows` of them).  A page number out of range among those that a row
+ * may see makes it, and may make other rows of its request, NaN
+ * (PHYAI_PAGED_BAD_PAGE).  Products of BF16 rows are accumulated in 32 bits;
+ * the probabilities enter the second product rounded to BF16. */
+int phyai_paged_attention(const phyai_paged_cache* cache, int32_t layer, const phyai_head_rows* q,
+                          const phyai_head_rows* out, const int32_t* kv_len, const int32_t* new_len,
+                          int32_t max_kv_len, float scale, int32_t causal, int32_t window, int32_t rows,
+                          int32_t dtype, void* workspace, int64_t workspace_bytes, int32_t* status, void* stream);
+
+/* Bytes of workspace that phyai_paged_attention needs with these arguments, or a
+ * negative phyai_status. */
+int64_t phyai_paged_attention_workspace(const phyai_paged_cache* cache, int32_t n_q_heads, int32_t rows,
+                                        int32_t max_kv_len);
+
+/* Copy the first kv_len[b] tokens of every request, all layers, into the contiguous
+ * prefix that phyai_denoise reads: out [n_layers][2][batch][rows][n_kv_heads *
+ * head_dim], F32 for an F32 cache, else BF16 (8-bit codes times their scale, rounded
+ * once).  Rows from kv_len[b] on are zero.  kv_len: device, 0 .. rows.  A request
+ * with a length out of range becomes NaN (PHYAI_PAGED_BAD_LENGTH), as do tokens
+ * of a page number out of range (PHYAI_PAGED_BAD_PAGE).  `out`: 16-byte aligned. */
+int phyai_paged_gather(const phyai_paged_cache* cache, const int32_t* kv_len, void* out, int32_t rows,
+                       int32_t* status, void* stream);
+
 /* Free every device buffer and graph of the handle.  NULL is accepted. */
 void phyai_free_expert(phyai_expert* e);
 

@@ -23,7 +23,8 @@ _DTYPE = {"f32": 0, "bf16": 1, "fp8": 2, "fp4": 3}
 # Every symbol include/phyai.h declares.
 EXPORTS = ("phyai_load_expert", "phyai_denoise", "phyai_denoise_static", "phyai_prepare", "phyai_debug_hidden",
            "phyai_profile_stage", "phyai_fp8_to_bf16", "phyai_free_expert", "phyai_last_error",
-           "phyai_version", "phyai_prefill", "phyai_encode_images")
+           "phyai_version", "phyai_prefill", "phyai_encode_images", "phyai_qk_norm_rope", "phyai_paged_append",
+           "phyai_paged_attention", "phyai_paged_attention_workspace", "phyai_paged_gather")
 STAGES = {"norm1": 0, "qkv": 1, "attn": 2, "oproj": 3, "norm2": 4, "mlp_up": 5, "mlp_down": 6}
 
 
@@ -47,6 +48,21 @@ class Tensor(ctypes.Structure):
                 ("cols", ctypes.c_int32), ("data", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
+class _HeadRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table")] + [
+        (n, ctypes.c_int64) for n in ("layer_stride", "page_stride", "token_stride", "head_stride")] + [
+        (n, ctypes.c_int32) for n in ("dtype", "n_layers", "n_kv_heads", "head_dim", "page_size", "n_pages", "batch",
+                                      "max_pages", "table_stride")]
+
+
+# bits of a status word (PHYAI_PAGED_*)
+PAGED_BAD_PAGE, PAGED_BAD_LENGTH = 1, 2
+
 _lib_handle = None
 
 
@@ -68,13 +84,21 @@ def lib() -> ctypes.CDLL:
         L.phyai_profile_stage.argtypes = [vp, i32, i32, vp]
         L.phyai_prefill.argtypes = [vp, vp, vp, vp, i32, vp]
         L.phyai_encode_images.argtypes = [vp, vp, vp, i32, i32, vp]
+        f32 = ctypes.c_float
+        L.phyai_qk_norm_rope.argtypes = [vp] * 6 + [f32, f32, vp, vp, i32, i32, i32, i32, vp, vp]
+        L.phyai_paged_append.argtypes = [vp, i32, vp, vp, f32, vp, vp, i32, i32, vp, vp]
+        L.phyai_paged_attention.argtypes = [vp, i32, vp, vp, vp, vp, i32, f32, i32, i32, i32, i32, vp, i64, vp, vp]
+        L.phyai_paged_attention_workspace.argtypes = [vp, i32, i32, i32]
+        L.phyai_paged_gather.argtypes = [vp, vp, vp, i32, vp, vp]
         L.phyai_free_expert.argtypes = [vp]
         L.phyai_free_expert.restype = None
         L.phyai_last_error.restype = ctypes.c_char_p
         for f in ("phyai_load_expert", "phyai_denoise", "phyai_denoise_static", "phyai_prepare", "phyai_debug_hidden",
                   "phyai_profile_stage", "phyai_fp8_to_bf16", "phyai_version", "phyai_prefill",
-                  "phyai_encode_images"):
+                  "phyai_encode_images", "phyai_qk_norm_rope", "phyai_paged_append", "phyai_paged_attention",
+                  "phyai_paged_gather"):
             getattr(L, f).restype = ctypes.c_int
+        L.phyai_paged_attention_workspace.restype = i64
         _lib_handle = L
     return _lib_handle
 
@@ -287,6 +311,246 @@ class VisionTower:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------------------
+# the paged key/value cache
+# ---------------------------------------------------------------------------
+def _dtype_of(t) -> int:
+    """F32, BF16 (or its bit patterns as int16) and FP8E4M3 (or its codes as uint8)."""
+    import torch
+    d = {torch.float32: 0, torch.bfloat16: 1, torch.int16: 1, torch.float8_e4m3fn: 2, torch.uint8: 2}.get(t.dtype)
+    if d is None:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return d
+
+
+def _head_rows(t, what: str, like=None) -> _HeadRows:
+    """[batch][rows][heads][head_dim] with any strides of the first three dimensions."""
+    if t.dim() != 4 or not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor [batch][rows][heads][head_dim]")
+    n, s = t.shape, t.stride()
+    if s[3] != 1:
+        raise ValueError(f"{what}: a head's values must be contiguous")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device or n[0] != like.shape[0] or
+                             n[1] != like.shape[1] or n[3] != like.shape[3]):
+        raise ValueError(f"{what}: batch, rows, head_dim, dtype and device must be those of the other rows")
+    # the stride of a dimension of one is nobody's
+    return _HeadRows(t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0, n[2])
+
+
+def _lengths(t, batch: int, like, what: str) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.dim() != 1 or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous int32 tensor on {like.device}")
+    if t.shape[0] < batch:
+        raise ValueError(f"{what}: shorter than the batch")
+    return t.data_ptr()
+
+
+def _floats(t, n: int, like, what: str) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != like.device or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{what}: expected {n} contiguous float32 values on {like.device}")
+    return t.data_ptr()
+
+
+def _status(t, like) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.device != like.device or t.numel() < 1:
+        raise ValueError(f"status: expected an int32 tensor on {like.device}")
+    return t.data_ptr()
+
+
+class _Device:
+    """The device of a call's tensors is current, and its outputs and workspace belong
+    to the call's stream, while the call is made.  The stream that is already
+    current needs neither."""
+
+    def __init__(self, t, stream):
+        import torch
+        self._guards = []
+        self._dev = t.device
+        if t.device.index != torch.cuda.current_device():
+            self._guards.append(torch.cuda.device(t.device))
+        if stream is not None:
+            if stream.device != t.device:
+                raise ValueError(f"the stream belongs to {stream.device}, the tensors to {t.device}")
+            self._guards.append(torch.cuda.stream(stream))
+
+    def __enter__(self) -> int:
+        import torch
+        for g in self._guards:
+            g.__enter__()
+        return torch.cuda.current_stream(self._dev).cuda_stream
+
+    def __exit__(self, *exc):
+        for g in reversed(self._guards):
+            g.__exit__(*exc)
+
+
+class PagedCache:
+    """Keys and values in pages (``phyai_paged_cache``): pools ``k`` and ``v`` of
+    [n_pages][page_size][n_kv_heads][head_dim], or with the layers in front, in any
+    order of the strides before the last dimension; ``page_table`` int32
+    [batch][max_pages].  float32, bfloat16 (or int16 bit patterns) or
+    float8_e4m3fn (or uint8 codes) with float32 ``k_scale`` and ``v_scale`` [n_kv_heads].
+
+    The tensors stay the caller's; the table may be rewritten between calls."""
+
+    def __init__(self, k, v, page_table, k_scale=None, v_scale=None):
+        import torch
+        if k.dim() not in (4, 5) or not k.is_cuda:
+            raise ValueError("expected device pools [layers][n_pages][page_size][n_kv_heads][head_dim]")
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must have the same shape, strides, dtype and device")
+        if k.stride(-1) != 1:
+            raise ValueError("a head's values must be contiguous")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != k.device:
+            raise ValueError(f"page_table: expected an int32 tensor [batch][max_pages] on {k.device}")
+        if page_table.shape[1] > 1 and page_table.stride(1) != 1:
+            raise ValueError("page_table: a request's entries must be contiguous")
+        dtype, n, s = _dtype_of(k), k.shape[-4:], k.stride()[-4:]
+        if (dtype == 2) != (k_scale is not None) or (dtype == 2) != (v_scale is not None):
+            raise ValueError("an 8-bit cache has k_scale and v_scale, another has none")
+        self.k, self.v, self.page_table, self.k_scale, self.v_scale = k, v, page_table, k_scale, v_scale
+        self.n_layers = k.shape[0] if k.dim() == 5 else 1
+        self.batch, self.page_size, self.n_kv_heads, self.head_dim = page_table.shape[0], n[1], n[2], n[3]
+        width = page_table.shape[1]
+        self._c = _PagedCache(
+            k.data_ptr(), v.data_ptr(), _floats(k_scale, n[2], k, "k_scale"), _floats(v_scale, n[2], k, "v_scale"),
+            page_table.data_ptr(), k.stride(0) if self.n_layers > 1 else 0, s[0] if n[0] > 1 else 0, s[1],
+            s[2] if n[2] > 1 else 0, dtype, self.n_layers, n[2], n[3], n[1], n[0], self.batch, width,
+            page_table.stride(0) if self.batch > 1 else width)
+        self._ref = ctypes.byref(self._c)
+
+    @property
+    def capacity(self) -> int:
+        """Tokens that a request's table has room for."""
+        return self.page_table.shape[1] * self.page_size
+
+
+def qk_norm_rope(q, k=None, q_gain=None, k_gain=None, *, eps: float = 1e-6, rope_base: float = 10000.0,
+                 past_len=None, new_len=None, q_out=None, k_out=None, status=None, stream=None):
+    """Norms of queries and keys for each head and their rotation in one pass
+    (``phyai_qk_norm_rope``).  q, k: [batch][rows][heads][head_dim]; q_gain, k_gain:
+    float32 [head_dim]; past_len, new_len: device int32 [batch].  eps = 0 only
+    rotates, rope_base = 0 only normalises.  Returns (q_out, k_out), new tensors
+    where none are given (their rows behind new_len are not written)."""
+    import torch
+    qs = _head_rows(q, "q")
+    ks = None if k is None else _head_rows(k, "k", q)
+    B, M, _, D = q.shape
+    with _Device(q, stream) as s:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif q_out.shape != q.shape:
+            raise ValueError("q_out: another shape than q")
+        if k is None:
+            if k_out is not None:
+                raise ValueError("k_out without k")
+        elif k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        elif k_out.shape != k.shape:
+            raise ValueError("k_out: another shape than k")
+        qo = _head_rows(q_out, "q_out", q)
+        ko = None if k is None else _head_rows(k_out, "k_out", q)
+        if B * M > 0:
+            _check(lib().phyai_qk_norm_rope(
+                ctypes.byref(qs), None if k is None else ctypes.byref(ks), ctypes.byref(qo),
+                None if k is None else ctypes.byref(ko), _floats(q_gain, D, q, "q_gain"),
+                _floats(k_gain, D, q, "k_gain"), eps, rope_base, _lengths(past_len, B, q, "past_len"),
+                _lengths(new_len, B, q, "new_len"), B, M, D, _dtype_of(q), _status(status, q), s))
+    return q_out, k_out
+
+
+def paged_append(cache: PagedCache, k, v, past_len, *, new_len=None, rope_base: float = 0.0, layer: int = 0,
+                 status=None, stream=None) -> None:
+    """Append keys and values [batch][rows][n_kv_heads][head_dim] of new tokens to the
+    cache at tokens past_len[b] .. past_len[b] + new_len[b] - 1, the keys rotated to
+    those positions where rope_base is not 0 (``phyai_paged_append``)."""
+    ks, vs = _head_rows(k, "k"), _head_rows(v, "v", k)
+    B, M, _, D = k.shape
+    if B != cache.batch or D != cache.head_dim or k.device != cache.k.device:
+        raise ValueError("k: batch, head_dim and device must be the cache's")
+    if B * M == 0:
+        return
+    with _Device(k, stream) as s:
+        _check(lib().phyai_paged_append(cache._ref, layer, ctypes.byref(ks), ctypes.byref(vs), rope_base,
+                                        _lengths(past_len, B, k, "past_len"), _lengths(new_len, B, k, "new_len"), M,
+                                        _dtype_of(k), _status(status, k), s))
+
+
+def paged_attention_workspace(cache: PagedCache, n_q_heads: int, rows: int, max_kv_len: Optional[int] = None) -> int:
+    """Bytes of workspace that such a ``paged_attention`` call needs."""
+    n = lib().phyai_paged_attention_workspace(cache._ref, n_q_heads, rows,
+                                              cache.capacity if max_kv_len is None else max_kv_len)
+    if n < 0:
+        _check(int(n))
+    return n
+
+
+def paged_attention(q, cache: PagedCache, kv_len, *, new_len=None, max_kv_len: Optional[int] = None,
+                    scale: Optional[float] = None, causal: bool = True, window: int = 0, layer: int = 0, out=None,
+                    workspace=None, status=None, stream=None):
+    """Attention of the last new_len[b] of a request's kv_len[b] cached tokens over all
+    of them (``phyai_paged_attention``).  q: [batch][rows][heads][head_dim]; kv_len,
+    new_len: device int32 [batch]; max_kv_len: the longest kv_len (default: what
+    the table has room for); scale: default 1 / sqrt(head_dim).  workspace: a
+    device tensor of at least ``paged_attention_workspace`` bytes (default: one is
+    allocated for the call).  Returns out (rows behind new_len are not written)."""
+    import torch
+    qs = _head_rows(q, "q")
+    B, M, H, D = q.shape
+    if B != cache.batch or D != cache.head_dim or q.device != cache.k.device:
+        raise ValueError("q: batch, head_dim and device must be the cache's")
+    if max_kv_len is None:
+        max_kv_len = cache.capacity
+    with _Device(q, stream) as s:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape:
+            raise ValueError("out: another shape than q")
+        if B * M == 0:
+            return out
+        os_ = _head_rows(out, "out", q)
+        need = paged_attention_workspace(cache, H, M, max_kv_len)
+        if workspace is None:
+            if need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        elif workspace.device != q.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on {q.device}")
+        _check(lib().phyai_paged_attention(
+            cache._ref, layer, ctypes.byref(qs), ctypes.byref(os_), _lengths(kv_len, B, q, "kv_len"),
+            _lengths(new_len, B, q, "new_len"), max_kv_len, D ** -0.5 if scale is None else scale, int(causal), window,
+            M, _dtype_of(q), None if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), _status(status, q), s))
+    return out
+
+
+def paged_gather(cache: PagedCache, kv_len, rows: int, *, out=None, status=None, stream=None):
+    """The first kv_len[b] tokens of every request and layer as the contiguous prefix
+    [layers][2][batch][rows][n_kv_heads * head_dim] that ``Expert.denoise`` reads
+    (``phyai_paged_gather``): float32 or bfloat16, zeros behind kv_len[b]."""
+    import torch
+    dt = torch.float32 if cache.k.dtype == torch.float32 else torch.bfloat16
+    shape = (cache.n_layers, 2, cache.batch, rows, cache.n_kv_heads * cache.head_dim)
+    with _Device(cache.k, stream) as s:
+        if out is None:
+            out = torch.empty(shape, dtype=dt, device=cache.k.device)
+        elif tuple(out.shape) != shape or out.dtype not in (dt, torch.int16 if dt == torch.bfloat16 else dt) or \
+                not out.is_contiguous() or out.device != cache.k.device:
+            raise ValueError(f"out: expected a contiguous {dt} tensor {shape} on {cache.k.device}")
+        if cache.batch * rows > 0:
+            _check(lib().phyai_paged_gather(cache._ref, _lengths(kv_len, cache.batch, cache.k, "kv_len"),
+                                            out.data_ptr(), rows, _status(status, cache.k), s))
+    return out
 
 
 def fp8_to_bf16(codes, stream=None):

@@ -16,7 +16,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libphyai.so")
 SOURCES = ["gemm.hip", "gemm_wide_store.hip", "gemm_wide_resid.hip", "gemm_wide_geglu.hip", "gemm_wide_qkv.hip",
-           "gemm_wide_kv.hip", "attention.hip", "rowops.hip", "runtime.hip", "persist.hip"]
+           "gemm_wide_kv.hip", "attention.hip", "rowops.hip", "runtime.hip", "persist.hip",
+           "paged_attention.hip", "paged_rows.hip", "paged_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

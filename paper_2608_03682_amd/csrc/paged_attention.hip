@@ -1,0 +1,751 @@
+// Attention of a chunk of new tokens, or of single tokens, over a paged
+// key/value cache.
+//
+// o_r = sum_j p_rj v_j, p_r = softmax_j(scale q_r . k_j) over the keys that row r
+// sees.  The query heads that share a K/V head are folded into the rows (row =
+// token * G + head of the group), so a K/V row is read once for all of them.
+//
+// MFMA formulation: S^T = K Q^T and O^T = V^T P^T on 32x32 tiles.  A query row is
+// always an MFMA column (lane % 32), its softmax state lives in lanes l and l ^ 32,
+// and the probabilities leave the S^T accumulators in the order in which the
+// P.V product takes them: accumulator v of lane half h is key 8 (v / 4) + 4 h + v % 4
+// of the 32, and the V^T operand is read in that same order.  V rows lie
+// token-major in their pages; the transposing LDS read hands each lane four keys of
+// one column.
+//
+// Two shapes of block:
+//   rows   NW waves x 32 query rows, K/V tiles shared by the waves: chunks, which
+//          are bound by the matrix cores and the exponentials;
+//   keys   every wave works on the same 32 rows and on key tiles of its own,
+//          joined in LDS at the end: few rows, which are bound by reading K/V.
+// Either may split the keys over blocks as well; a second kernel joins the splits.
+#include "common.hpp"
+#include "errors.hpp"
+#include "paged.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace phyai {
+
+namespace {
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// LDS by byte address
+template <typename V>
+__device__ __forceinline__ V lds_at(uint32_t addr) {
+  return *reinterpret_cast<__attribute__((address_space(3))) const V*>(addr);
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 16 bytes per lane from base + off into LDS at (wave-uniform) lds + 16 * lane.
+// `base` is wave-uniform.  Completion is awaited with dma_wait.
+__device__ __forceinline__ void dma16(const char* base, uint32_t off, uint32_t lds) {
+  // the halves are cast to 32 unsigned bits before they are widened: readfirstlane
+  // returns an int, whose sign would spread over the upper half
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  const uint32_t p_lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p));
+  const uint32_t p_hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p >> 32));
+  const uint64_t sp = static_cast<uint64_t>(p_hi) << 32 | p_lo;
+  lds = __builtin_amdgcn_readfirstlane(lds);
+  // a vector instruction may have written the base just before: five wait states to
+  // the load that reads it, which the compiler does not count inside asm
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(lds), "v"(off), "s"(sp) : "memory", "m0");
+}
+__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Barrier without the fence of __syncthreads(): the caller's LDS accesses are
+// complete (lgkmcnt 0), loads into LDS have been awaited before.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// The larger value, NaN if either is (one v_maximum3_f32 for two of them; fmaxf would
+// quiet every input first).  Left to the compiler and not written as asm: it counts
+// the wait states between a matrix instruction and the first reader of its result.
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float max3(float a, float b, float c) { return max2(max2(a, b), c); }
+__device__ __forceinline__ float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// LDS tiles hold rows of RB bytes in 16-byte chunks, chunk c of row r at
+// c ^ swz(r), so that the lanes of one fragment read fall in different banks:
+//   K   16 lanes read 16 consecutive rows at one chunk
+//   V   bf16: 16 lanes read 32 bytes of each of 4 rows, the other lane half the
+//       next 4 rows; f32: 32 lanes read 128 bytes of one row, the other half of
+//       the row 4 further on
+template <int RB>
+__device__ __forceinline__ int k_swz(int r) { return RB >= 256 ? (r & 15) : ((r >> 1) & 7); }
+template <int ES, int RB>
+__device__ __forceinline__ int v_swz(int r) {
+  if (ES == 4) return 8 * ((r >> 2) & 1);
+  return RB >= 256 ? 2 * (r & 7) : 2 * ((r >> 1) & 3);
+}
+
+// Order of one MFMA loop whose operands come from LDS: PD reads ahead, then each
+// MFMA followed by the reads of a later one (RPM reads per MFMA).
+template <int N, int RPM, int PD>
+__device__ __forceinline__ void mfma_pipeline() {
+#pragma unroll
+  for (int i = 0; i < PD; ++i) __builtin_amdgcn_sched_group_barrier(0x100, RPM, 0);
+#pragma unroll
+  for (int i = 0; i < N - PD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, RPM, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < PD; ++i) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+}
+
+__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+
+// What a block of one kind looks like.  CT: element of the pool, T: of the rows
+// and of the products.
+template <typename CT, typename T, int D, bool KEYS>
+struct Shape {
+  static constexpr int ES = sizeof(T);
+  static constexpr bool kFp8 = sizeof(CT) == 1;
+  static constexpr int RB = D * ES;                     // bytes of an LDS row
+  static constexpr int CPR = RB / 16;                   // chunks of a row
+  static constexpr int KT = (ES == 2 && !KEYS) ? 64 : 32;   // keys of a tile
+  static constexpr int TILE = KT * RB;                  // bytes of a K or V tile
+  // keys: as many waves as 128 KiB of double-buffered tiles allow, at most 4
+  static constexpr int NW = KEYS ? (4 * TILE * 4 <= 128 * 1024 ? 4 : (4 * TILE * 2 <= 128 * 1024 ? 2 : 1)) : 4;
+  static constexpr int ROWS = KEYS ? 32 : 32 * NW;      // query rows of a block
+  static constexpr int SETS = KEYS ? NW : 1;            // tile sets
+  static constexpr int LDS = SETS * 4 * TILE;           // [set][buffer][K, V]
+  static constexpr int STEP = KEYS ? NW * KT : KT;      // keys of one turn of the loop
+  // blocks of a CU that LDS and registers allow; also the waves of a SIMD asked for
+  static constexpr int PER_CU = KEYS ? (LDS <= 64 * 1024 ? 2 : 1) : (LDS <= 64 * 1024 ? 2 : 1);
+};
+
+template <typename CT, typename T, int D, bool KEYS, int NT = 64 * Shape<CT, T, D, KEYS>::NW,
+          int PER_SIMD = Shape<CT, T, D, KEYS>::PER_CU>
+__global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs a) {
+  using S = Shape<CT, T, D, KEYS>;
+  constexpr int ES = S::ES, RB = S::RB, CPR = S::CPR, KT = S::KT, KB = KT / 32, TILE = S::TILE, NW = S::NW;
+  constexpr int ROWS = S::ROWS, NQ = RB / 32;           // chunk pairs of a row
+  // aligned so that the two buffers of a tile differ in one address bit
+  __shared__ __attribute__((aligned(2 * TILE))) char sm[S::LDS];
+  __shared__ float s_ml[NW][32][2];
+  __shared__ uint32_t s_nan;
+  __shared__ int s_bad;
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int lr = lane % 32, hl = lane / 32;
+  const int G = a.G;
+
+  // Blocks are dealt to the 8 XCDs in turn; each XCD takes a run of (request, K/V
+  // head, split) groups, whose keys its L2 then holds.  Inside a group the tiles
+  // alternate between the last (under a causal mask the longest) and the first,
+  // so that any part of a group is about as much work.
+  const int total = a.B * a.nkv * a.n_split * a.n_tiles;
+  const int per_xcd = (total + 7) / 8;
+  const int wid = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (wid >= total) return;
+  const int gi = wid / a.n_tiles, tp = wid % a.n_tiles;
+  const int rt = (tp & 1) ? tp / 2 : a.n_tiles - 1 - tp / 2;
+  const int grp = gi / a.n_split, split = gi % a.n_split;
+  const int b = grp / a.nkv, kvh = grp % a.nkv;
+
+  // readfirstlane: the compiler keeps what it loads as vectors, and everything that
+  // follows from the lengths would be vector arithmetic and divergent branches
+  int kv = __builtin_amdgcn_readfirstlane(a.kv_len[b]);
+  const RowSpan span = row_span(a.new_len ? __builtin_amdgcn_readfirstlane(a.new_len[b]) : a.M, 0, a.M, a.M);
+  bool bad = !span.ok || kv < 0 || kv > a.max_kv;
+  if (bad) {
+    kv = 0;
+    if (a.status && threadIdx.x == 0) atomicOr(a.status, PAGED_BAD_LENGTH);
+  }
+  const int n = span.n, rows = n * G;
+  if (rt * ROWS >= rows) return;
+
+  if (threadIdx.x == 0) {
+    s_nan = 0;
+    s_bad = 0;
+  }
+  __syncthreads();
+
+  // this lane's query row and the keys it sees; a lane behind the last row works on
+  // zeros and sees what the others see
+  const int wrow = rt * ROWS + (KEYS ? 0 : wave * 32);
+  const int row = wrow + lr;
+  const bool valid = row < rows;
+  const int tok = valid ? row / G : n - 1;
+  const int qhead = kvh * G + (valid ? row % G : 0);
+  const int hi = seen_end(tok, n, kv, a.causal), lo = seen_begin(tok, n, kv, a.window);
+
+  // Q^T operand: chunk 2 s + h of the row
+  uint4 qf[NQ];
+  {
+    const char* qp = static_cast<const char*>(a.q.p) + (b * a.q.b + tok * a.q.t + qhead * a.q.h) * ES + 16 * hl;
+#pragma unroll
+    for (int s = 0; s < NQ; ++s) {
+      qf[s] = make_uint4(0, 0, 0, 0);
+      if (valid) qf[s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
+    }
+  }
+
+  // keys of the block, of this split and of this wave's rows
+  const int tok0 = (rt * ROWS) / G, tok1 = min(n - 1, (rt * ROWS + ROWS - 1) / G);
+  const int bl = seen_begin(tok0, n, kv, a.window) / KT * KT, bh = seen_end(tok1, n, kv, a.causal);
+  int kbeg = bl, kend = bh;
+  if (a.n_split > 1) {
+    const int steps = bh > bl ? (bh - bl + S::STEP - 1) / S::STEP : 0;
+    const int per = (steps + a.n_split - 1) / a.n_split * S::STEP;
+    kbeg = bl + split * per;
+    kend = min(bh, kbeg + per);
+  }
+  const int wl = seen_begin(min(wrow / G, n - 1), n, kv, a.window);
+  const int wh = wrow < rows ? seen_end(min(n - 1, (wrow + 31) / G), n, kv, a.causal) : 0;
+
+  const float ks = S::kFp8 ? a.pool.k_scale[kvh] : 1.f;
+  const float vs = S::kFp8 ? a.pool.v_scale[kvh] : 1.f;
+  const float sl2 = fmaxf(a.scale * ks * kLog2e, 1e-37f);  // not 0: a hidden key's -inf stays -inf
+
+  // ---- loading ----
+  // LDS: [set][K, V][buffer][TILE]; addresses of the two buffers differ in one bit
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)sm)) + (KEYS ? wave : 0) * 4 * TILE;
+  const int psm = (1 << a.pool.page_shift) - 1;
+  const int32_t* table = a.pool.table + (int64_t)b * a.pool.table_stride;
+  const char* kpool = a.pool.k + kvh * a.pool.head_bytes;
+  const char* vpool = a.pool.v + kvh * a.pool.head_bytes;
+  const int last_page = (kend - 1) >> a.pool.page_shift;
+  // 64 entries of the table from `pbase` on, one per lane; the numbers are checked here
+  int pbase = 0, pages = 0;
+  auto load_pages = [&](int from) {
+    pbase = from;
+    const int i = from + lane;
+    int id = 0;
+    if (i <= last_page && i < a.pool.max_pages) id = table[i];
+    const bool out = !page_ok(id, a.pool.n_pages);
+    if (__ballot(out)) {
+      bad = true;
+      if (a.status && lane == 0) atomicOr(a.status, PAGED_BAD_PAGE);
+    }
+    pages = out ? 0 : id;
+  };
+  auto page_of = [&](int key) { return __builtin_amdgcn_readlane(pages, (key >> a.pool.page_shift) - pbase); };
+
+  constexpr int GB = S::kFp8 ? D : RB;                  // bytes of a row in its page
+  constexpr int LPR = GB / 16;                          // lanes of a row
+  constexpr int RPI = kWave / LPR;                      // rows of one load instruction
+  constexpr int NLD = KT / RPI / (KEYS ? 1 : NW);       // load instructions of a wave, per operand
+  static_assert(KT % RPI == 0 && (KEYS || KT / RPI % NW == 0) && NLD >= 1, "whole loads");
+  static_assert(RPI <= 16, "the rows of one load lie in one page");
+  // Row first_row(i) + lane / LPR, chunk lane % LPR.  A lane's place in its row is
+  // chunk ^ swizzle; what of the swizzle depends on i is a constant, since
+  // first_row(i) and lane / LPR share no bits.
+  const int lrow = lane / LPR, wrow0 = (KEYS ? 0 : wave) * RPI;
+  auto row_of = [&](int i) { return (KEYS ? i : NW * i) * RPI; };   // first_row(i) - wrow0
+  const uint32_t lane_row = static_cast<uint32_t>(lrow) * a.pool.token_bytes;
+  const uint32_t kc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : k_swz<RB>(wrow0 + lrow)));
+  const uint32_t vc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : v_swz<ES, RB>(wrow0 + lrow)));
+  uint4 kr[S::kFp8 ? NLD : 1], vr[S::kFp8 ? NLD : 1];
+  auto issue = [&](uint32_t buf, int k0) {
+    const int lastp = min(k0 + KT - 1, kend - 1) >> a.pool.page_shift;
+    if (lastp >= pbase + kWave) load_pages(k0 >> a.pool.page_shift);
+    const bool whole = k0 + KT <= kend;
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) {
+      const int r0 = wrow0 + row_of(i);
+      const int key = min(k0 + r0, kend - 1);
+      int64_t base = (int64_t)page_of(key) * a.pool.page_bytes;
+      uint32_t ro = lane_row;
+      if (whole) {
+        base += (int64_t)((k0 + r0) & psm) * a.pool.token_bytes;
+      } else {
+        // the range ends inside the tile: lanes behind it read its last key again
+        ro = static_cast<uint32_t>(min(k0 + r0 + lrow, kend - 1) & psm) * a.pool.token_bytes;
+      }
+      const uint32_t ko = ro + (kc ^ (S::kFp8 ? 0 : 16 * k_swz<RB>(row_of(i))));
+      const uint32_t vo = ro + (vc ^ (S::kFp8 ? 0 : 16 * v_swz<ES, RB>(row_of(i))));
+      if constexpr (S::kFp8) {
+        kr[i] = *reinterpret_cast<const uint4*>(kpool + base + ko);
+        vr[i] = *reinterpret_cast<const uint4*>(vpool + base + vo);
+      } else {
+        dma16(kpool + base, ko, lds0 + buf + r0 * RB);
+        dma16(vpool + base, vo, lds0 + buf + 2 * TILE + r0 * RB);
+      }
+    }
+  };
+  // the loads of the next tile are complete and in LDS
+  auto commit = [&](uint32_t buf) {
+    if constexpr (S::kFp8) {
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        const int r = wrow0 + row_of(i) + lrow, c = 2 * (lane % LPR);
+        char* kt = sm + (KEYS ? wave : 0) * 4 * TILE + buf + r * RB;
+        char* vt = kt + 2 * TILE;
+        *reinterpret_cast<bf16x8*>(kt + 16 * (c ^ k_swz<RB>(r))) = fp8x8_to_bf16x8(kr[i].x, kr[i].y);
+        *reinterpret_cast<bf16x8*>(kt + 16 * ((c + 1) ^ k_swz<RB>(r))) = fp8x8_to_bf16x8(kr[i].z, kr[i].w);
+        *reinterpret_cast<bf16x8*>(vt + 16 * (c ^ v_swz<ES, RB>(r))) = fp8x8_to_bf16x8(vr[i].x, vr[i].y);
+        *reinterpret_cast<bf16x8*>(vt + 16 * ((c + 1) ^ v_swz<ES, RB>(r))) = fp8x8_to_bf16x8(vr[i].z, vr[i].w);
+      }
+    } else {
+      dma_wait();
+    }
+    // keys: other lanes of this wave read what was written here; LDS operations of a
+    // wave complete in order, the compiler has to keep that order.  rows: the
+    // barrier publishes the tile and tells that everybody is done with the other.
+    if constexpr (KEYS) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+
+  // ---- one tile ----
+  f32x16 o[D / 32];
+  float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+
+  // Fragment addresses: chunk 2 s + h of K row lr is at k_at ^ 32 s, the V^T operand
+  // of dims 32 db + lr in the key order of the accumulators at v_at ^ (64 db) (bf16,
+  // four keys a read) or v_at ^ (128 db) (f32, one key), plus whole rows.
+  const int i16 = lane % 16, vr0 = ES == 2 ? 4 * hl + i16 / 4 : 4 * hl;
+  const uint32_t k_at = lds0 + lr * RB + 16 * (hl ^ k_swz<RB>(lr));
+  const uint32_t v_at =
+      lds0 + 2 * TILE + vr0 * RB +
+      (ES == 2 ? 16 * ((2 * ((lane / 16) % 2) + (i16 % 4) / 2) ^ v_swz<ES, RB>(vr0)) + 8 * (i16 & 1)
+               : 16 * ((lr / 4) ^ v_swz<ES, RB>(vr0)) + 4 * (lr % 4));
+  auto v_bf16 = [&](uint32_t at, int t, int db) {
+    union { s16x4 h[2]; bf16x8 v; } f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      f.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          reinterpret_cast<__attribute__((address_space(3))) s16x4*>((at ^ (64u * db)) + (16 * t + 8 * j) * RB));
+    return f.v;
+  };
+  auto v_f32 = [&](uint32_t at, int kb, int v, int db) {
+    return lds_at<float>((at ^ (128u * db)) + (32 * kb + 8 * (v / 4) + v % 4) * RB);
+  };
+
+  auto compute = [&](uint32_t buf, int k0) {
+    const uint32_t ka = k_at ^ buf, tv = v_at ^ buf;
+    f32x16 st[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) st[kb][v] = 0.f;
+#pragma unroll
+    for (int s = 0; s < NQ; ++s)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const u32x4 kv4 = lds_at<u32x4>((ka ^ (32u * s)) + 32 * kb * RB);
+        const uint4 kf = make_uint4(kv4.x, kv4.y, kv4.z, kv4.w);
+        if constexpr (ES == 2) {
+          st[kb] = mfma32x32x16(as_bf16x8(kf), as_bf16x8(qf[s]), st[kb]);
+        } else {
+          st[kb] = mfma_f32(__uint_as_float(kf.x), __uint_as_float(qf[s].x), st[kb]);
+          st[kb] = mfma_f32(__uint_as_float(kf.y), __uint_as_float(qf[s].y), st[kb]);
+          st[kb] = mfma_f32(__uint_as_float(kf.z), __uint_as_float(qf[s].z), st[kb]);
+          st[kb] = mfma_f32(__uint_as_float(kf.w), __uint_as_float(qf[s].w), st[kb]);
+        }
+      }
+    if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
+    // hidden keys get -inf, only in tiles where a row of the wave has any
+    const bool need_mask = __ballot(k0 < lo || k0 + KT > hi) != 0;
+    if (need_mask) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int key = k0 + 32 * kb + 8 * (v / 4) + 4 * hl + v % 4;
+          st[kb][v] = key >= lo && key < hi ? st[kb][v] : -INFINITY;
+        }
+    }
+    float mx[2 * KB];
+#pragma unroll
+    for (int c = 0; c < 2 * KB; ++c) {
+      const f32x16& x = st[c >> 1];
+      const int f = 8 * (c & 1);
+      float m = max3(x[f], x[f + 1], x[f + 2]);
+      m = max3(m, x[f + 3], x[f + 4]);
+      m = max3(m, x[f + 5], x[f + 6]);
+      mx[c] = max2(m, x[f + 7]);
+    }
+    float tmax = max2(mx[0], mx[1]);
+    if constexpr (KB == 2) tmax = max3(tmax, mx[2], mx[3]);
+    tmax = pair_max(tmax) * sl2;
+    // The reference m moves only when a tile's maximum exceeds it by more than 8
+    // (powers of two: p stays below 2^8), so the accumulators are rescaled a few
+    // times per key range and not at every tile.
+    if (__ballot(tmax > m_run + 8.f)) {
+      const float m_new = fmaxf(m_run, tmax);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) o[i] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every p is 0
+    float ps[2 * KB];
+    bf16x8 pf[2 * KB];
+#pragma unroll
+    for (int t = 0; t < 2 * KB; ++t) {
+      float pv[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        pv[j] = __builtin_amdgcn_exp2f(fmaf(st[t >> 1][8 * (t & 1) + j], sl2, -m_use));
+        if constexpr (ES == 4) st[t >> 1][8 * (t & 1) + j] = pv[j];
+      }
+      ps[t] = ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
+      if constexpr (ES == 2) {
+        uint4 w;
+        w.x = pack_bf16x2(pv[0], pv[1]);
+        w.y = pack_bf16x2(pv[2], pv[3]);
+        w.z = pack_bf16x2(pv[4], pv[5]);
+        w.w = pack_bf16x2(pv[6], pv[7]);
+        pf[t] = as_bf16x8(w);
+      }
+    }
+    if constexpr (KB == 2) l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+    else l_run += ps[0] + ps[1];
+    if constexpr (ES == 2) {
+#pragma unroll
+      for (int t = 0; t < 2 * KB; ++t)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) o[db] = mfma32x32x16(v_bf16(tv, t, db), pf[t], o[db]);
+      mfma_pipeline<2 * KB * (D / 32), 2, 2>();
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) o[db] = mfma_f32(v_f32(tv, kb, v, db), st[kb][v], o[db]);
+    }
+  };
+
+  // ---- the key range ----
+  int k0 = kbeg + (KEYS ? wave * KT : 0);
+  if (k0 < kend) {
+    // two buffers: the next tile is under way while this one is worked on
+    uint32_t buf = 0;
+    load_pages(k0 >> a.pool.page_shift);
+    issue(0, k0);
+    commit(0);
+    if constexpr (!KEYS) lds_barrier();
+    for (;;) {
+      const int next = k0 + S::STEP;
+      const bool more = next < kend;
+      if (more) issue(buf ^ TILE, next);
+      if (KEYS || (k0 < wh && k0 + KT > wl)) compute(buf, k0);
+      if (more) commit(buf ^ TILE);
+      if constexpr (!KEYS) lds_barrier();
+      if (!more) break;
+      k0 = next;
+      buf ^= TILE;
+    }
+  }
+  l_run = pair_sum(l_run);
+
+  // A hidden key's weight is 0, and 0 times an infinite or NaN value is NaN: rows that
+  // came out NaN although their weights are numbers are computed once more, over the
+  // keys that they see and no other, with the maximum m and sum l found above.
+  float nan = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) nan += o[i][v];
+  const uint64_t nan_lanes = __ballot(valid && nan != nan && l_run == l_run);
+  const uint32_t nan_rows = static_cast<uint32_t>(nan_lanes) | static_cast<uint32_t>(nan_lanes >> 32);
+  const int64_t grow = (int64_t)grp * a.M * G;          // first row of (request, K/V head) in the workspace
+  auto repair = [&](int rr, float m, float l) {
+    constexpr int E = D / kWave;
+    const int t = rr / G;
+    const int64_t head = kvh * G + rr % G;
+    const T* qp = static_cast<const T*>(a.q.p) + b * a.q.b + t * a.q.t + head * a.q.h + E * lane;
+    float q[E], acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      q[e] = ActIO<T>::load(qp + e);
+      acc[e] = 0.f;
+    }
+    auto elem = [](const char* p, int e) {
+      if constexpr (S::kFp8) return __uint_as_float(fp8x2_to_bf16x2<false>(reinterpret_cast<const uint8_t*>(p)[e]) << 16);
+      else return ActIO<T>::load(reinterpret_cast<const T*>(p) + e);
+    };
+    const int end = min(kend, seen_end(t, n, kv, a.causal));
+    for (int key = max(kbeg, seen_begin(t, n, kv, a.window)); key < end; ++key) {
+      const int id = table[key >> a.pool.page_shift];
+      if (!page_ok(id, a.pool.n_pages)) continue;       // such a block is NaN in any case
+      const int64_t at = page_row_offset(a.pool, id, key, kvh) + (int64_t)E * lane * sizeof(CT);
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) s = fmaf(q[e], elem(a.pool.k + at, e), s);
+      const float p = __builtin_amdgcn_exp2f(fmaf(wave_sum(s), sl2, -m));
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(p, elem(a.pool.v + at, e), acc[e]);
+    }
+    if (a.n_split == 1) {
+      T* op = static_cast<T*>(a.out.p) + b * a.out.b + t * a.out.t + head * a.out.h + E * lane;
+#pragma unroll
+      for (int e = 0; e < E; ++e) ActIO<T>::store(op + e, acc[e] * (vs / l));
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) a.part[((grow + rr) * a.n_split + split) * D + E * lane + e] = acc[e];
+    }
+  };
+
+  // ---- out ----
+  // an unusable page or length makes the block's rows NaN
+  if (bad && lane == 0) s_bad = 1;
+  __syncthreads();
+  bad = __builtin_amdgcn_readfirstlane(s_bad) != 0;
+  if (bad) {
+    m_run = 0.f;
+    l_run = __builtin_nanf("");
+  }
+  if constexpr (KEYS) {
+    // the waves' parts, chunk c of row r at c ^ (r % 16)
+    float* so = reinterpret_cast<float*>(sm) + wave * 32 * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = 8 * db + 2 * u + hl;
+        *reinterpret_cast<float4*>(so + lr * D + 4 * (c ^ (lr & 15))) =
+            make_float4(o[db][4 * u], o[db][4 * u + 1], o[db][4 * u + 2], o[db][4 * u + 3]);
+      }
+    if (hl == 0) {
+      s_ml[wave][lr][0] = m_run;
+      s_ml[wave][lr][1] = l_run;
+    }
+    if (nan_rows && lane == 0) atomicOr(&s_nan, nan_rows);
+    __syncthreads();
+    const int live = min(32, rows - wrow);
+    for (int x = threadIdx.x; x < live * (D / 4); x += 64 * NW) {
+      const int r = x / (D / 4), c = x % (D / 4);
+      float mm = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) mm = fmaxf(mm, s_ml[w][r][0]);
+      float l = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float lw = s_ml[w][r][1];
+        const float f = lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_ml[w][r][0] - mm);
+        if (lw != 0.f) {
+          const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<float*>(sm) + (w * 32 + r) * D +
+                                                            4 * (c ^ (r & 15)));
+          acc.x = fmaf(f, v.x, acc.x);
+          acc.y = fmaf(f, v.y, acc.y);
+          acc.z = fmaf(f, v.z, acc.z);
+          acc.w = fmaf(f, v.w, acc.w);
+          l = fmaf(f, lw, l);
+        }
+      }
+      const int rr = wrow + r;
+      if (a.n_split == 1) {
+        const float inv = l == 0.f ? 0.f : vs / l;
+        const float v4[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+        T* op = static_cast<T*>(a.out.p) + b * a.out.b + (rr / G) * a.out.t + (kvh * G + rr % G) * a.out.h + 4 * c;
+        ActIO<T>::store4(op, v4);
+      } else {
+        const int64_t at = (grow + rr) * a.n_split + split;
+        *reinterpret_cast<float4*>(a.part + at * D + 4 * c) = acc;
+        if (c == 0) a.ml[at] = make_float2(mm, l);
+      }
+    }
+    const uint32_t redo = __builtin_amdgcn_readfirstlane(s_nan);
+    if (redo && !bad) {
+      __syncthreads();                                  // the rows above are written
+      for (int r = wave; r < 32; r += NW) {
+        if (!(redo >> r & 1)) continue;
+        float mm = -INFINITY, l = 0.f;
+        for (int w = 0; w < NW; ++w) mm = fmaxf(mm, s_ml[w][r][0]);
+        for (int w = 0; w < NW; ++w)
+          if (s_ml[w][r][1] != 0.f) l = fmaf(__builtin_amdgcn_exp2f(s_ml[w][r][0] - mm), s_ml[w][r][1], l);
+        repair(wrow + r, mm, l);
+      }
+    }
+  } else if (a.n_split > 1) {
+    if (valid) {
+      const int64_t at = (grow + row) * a.n_split + split;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<float4*>(a.part + at * D + 32 * db + 8 * u + 4 * hl) =
+              make_float4(o[db][4 * u], o[db][4 * u + 1], o[db][4 * u + 2], o[db][4 * u + 3]);
+      if (hl == 0) a.ml[at] = make_float2(m_run, l_run);
+    }
+  } else {
+    // whole rows through LDS, so that a store instruction covers 1 KiB of them
+    const float inv = l_run == 0.f ? 0.f : vs / l_run;
+    char* stage = sm + wave * 32 * RB;
+    static_assert(S::LDS >= NW * 32 * RB, "the output is staged in the tiles");
+    constexpr int SW = CPR < 16 ? CPR - 1 : 15;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float v4[4] = {o[db][4 * u] * inv, o[db][4 * u + 1] * inv, o[db][4 * u + 2] * inv, o[db][4 * u + 3] * inv};
+        const int byte = (32 * db + 8 * u + 4 * hl) * ES;
+        ActIO<T>::store4(reinterpret_cast<T*>(stage + lr * RB + 16 * ((byte / 16) ^ (lr & SW)) + byte % 16), v4);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int RPS = kWave / CPR > 0 ? kWave / CPR : 1;
+#pragma unroll
+    for (int i = 0; i < 32 / RPS; ++i) {
+      const int r = RPS * i + lane / CPR, c = lane % CPR;
+      const int rr = wrow + r;
+      if (rr < rows) {
+        const uint4 w = *reinterpret_cast<const uint4*>(stage + r * RB + 16 * (c ^ (r & SW)));
+        char* op = reinterpret_cast<char*>(static_cast<T*>(a.out.p) + b * a.out.b + (rr / G) * a.out.t +
+                                           (kvh * G + rr % G) * a.out.h);
+        *reinterpret_cast<uint4*>(op + 16 * c) = w;
+      }
+    }
+  }
+  if constexpr (!KEYS) {
+    if (nan_rows && !bad) {
+      dma_wait();                                       // the rows above are written
+      for (uint32_t left = nan_rows; left; left &= left - 1) {
+        const int r = __builtin_ctz(left);
+        repair(wrow + r, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m_run), r)),
+               __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_run), r)));
+      }
+    }
+  }
+}
+
+// Joins the splits of one row per wave: o = sum_s w_s o_s / sum_s w_s l_s, w_s =
+// 2^(m_s - max m), in the order of the splits.  Splits without a key have l = 0
+// and are not read.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, bool fp8) {
+  constexpr int E = D / kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int MG = a.M * a.G;
+  const int64_t gr = (int64_t)blockIdx.x * 4 + wave;
+  if (gr >= (int64_t)a.B * a.nkv * MG) return;
+  const int grp = static_cast<int>(gr / MG), row = static_cast<int>(gr % MG);
+  const int b = grp / a.nkv, kvh = grp % a.nkv;
+  const RowSpan span = row_span(a.new_len ? a.new_len[b] : a.M, 0, a.M, a.M);
+  if (row >= span.n * a.G) return;
+  const float2* ml = a.ml + gr * a.n_split;
+  float m = -INFINITY, l = 0.f;
+  if (lane < a.n_split) {
+    const float2 x = ml[lane];
+    m = x.x;
+    l = x.y;
+  }
+  float mm = m;
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) mm = fmaxf(mm, __shfl_xor(mm, s, kWave));
+  const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - mm);
+  const float total = wave_sum(l == 0.f ? 0.f : w * l);
+  float acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  const float* part = a.part + gr * a.n_split * D + E * lane;
+  for (int s = 0; s < a.n_split; ++s) {
+    const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
+    const float lsp = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l), s));
+    if (lsp == 0.f) continue;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = fmaf(ws, part[(int64_t)s * D + e], acc[e]);
+  }
+  const float inv = total == 0.f ? 0.f : (fp8 ? a.pool.v_scale[kvh] : 1.f) / total;
+  T* op = static_cast<T*>(a.out.p) + b * a.out.b + (row / a.G) * a.out.t + (kvh * a.G + row % a.G) * a.out.h + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) ActIO<T>::store(op + e, acc[e] * inv);
+}
+
+// Few rows: every wave reads keys of its own.  More than 64 rows of a K/V head would
+// read the keys three times and more.
+bool keys_shape(const PagedAttnArgs& a) { return a.M * a.G <= 64; }
+
+template <typename CT, typename T, int D, bool KEYS>
+void launch(const PagedAttnArgs& a, hipStream_t s) {
+  const int64_t total = (int64_t)a.B * a.nkv * a.n_split * a.n_tiles;
+  const int grid = static_cast<int>((total + 7) / 8 * 8);
+  paged_attn_kernel<CT, T, D, KEYS><<<grid, 64 * Shape<CT, T, D, KEYS>::NW, 0, s>>>(a);
+  if (a.n_split > 1) {
+    const int64_t rows = (int64_t)a.B * a.nkv * a.M * a.G;
+    paged_join_kernel<T, D><<<static_cast<int>((rows + 3) / 4), 256, 0, s>>>(a, sizeof(CT) == 1);
+  }
+}
+
+template <typename CT, typename T, int D>
+void launch_shape(const PagedAttnArgs& a, hipStream_t s) {
+  if (keys_shape(a)) launch<CT, T, D, true>(a, s);
+  else launch<CT, T, D, false>(a, s);
+}
+
+template <typename CT, typename T, int D, bool KEYS>
+void plan(PagedAttnArgs& a) {
+  using S = Shape<CT, T, D, KEYS>;
+  a.n_tiles = (a.M * a.G + S::ROWS - 1) / S::ROWS;
+  const int64_t base = (int64_t)a.B * a.nkv * a.n_tiles;
+  const int64_t slots = 256 * S::PER_CU;
+  const int steps = std::max(1, (a.max_kv + S::STEP - 1) / S::STEP);
+  // A block costs its steps plus about one to start and one to finish, a launch the
+  // rounds of its blocks over the chip, joining about two steps.
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int n = 1; n <= std::min(64, steps); ++n) {
+    const int per = (steps + n - 1) / n;
+    if ((steps + per - 1) / per != n) continue;         // the last splits would be empty
+    const int64_t cost = (base * n + slots - 1) / slots * (per + 2) + (n > 1 ? 2 : 0);
+    if (cost < least) {
+      least = cost;
+      best = n;
+    }
+    if (base * n >= 4 * slots) break;
+  }
+  a.n_split = best;
+}
+
+template <typename CT, typename T, int D>
+void plan_shape(PagedAttnArgs& a) {
+  if (keys_shape(a)) plan<CT, T, D, true>(a);
+  else plan<CT, T, D, false>(a);
+}
+
+template <typename F>
+void by_dim(int D, F&& f) {
+  switch (D) {
+    case 64: f(std::integral_constant<int, 64>{}); break;
+    case 128: f(std::integral_constant<int, 128>{}); break;
+    default: f(std::integral_constant<int, 256>{}); break;
+  }
+}
+
+}  // namespace
+
+int64_t paged_attention_plan(PagedAttnArgs& a, int D, int pool_kind) {
+  by_dim(D, [&](auto d) {
+    constexpr int kD = decltype(d)::value;
+    if (pool_kind == PAGED_F32) plan_shape<float, float, kD>(a);
+    else if (pool_kind == PAGED_BF16) plan_shape<bf16_t, bf16_t, kD>(a);
+    else plan_shape<uint8_t, bf16_t, kD>(a);
+  });
+  if (a.n_split == 1) return 0;
+  return (int64_t)a.B * a.nkv * a.M * a.G * a.n_split * (D + 2);
+}
+
+void paged_attention(const PagedAttnArgs& a, int D, int pool_kind, hipStream_t s) {
+  by_dim(D, [&](auto d) {
+    constexpr int kD = decltype(d)::value;
+    if (pool_kind == PAGED_F32) launch_shape<float, float, kD>(a, s);
+    else if (pool_kind == PAGED_BF16) launch_shape<bf16_t, bf16_t, kD>(a, s);
+    else launch_shape<uint8_t, bf16_t, kD>(a, s);
+  });
+}
+
+}  // namespace phyai

@@ -18,25 +18,12 @@
 #include <vector>
 
 #include "../../include/phyai.h"
+#include "errors.hpp"
 #include "kernels.hpp"
 
 using namespace phyai;
 
 namespace {
-
-thread_local std::string g_err;
-
-struct Fail {
-  int code;
-  std::string msg;
-};
-
-[[noreturn]] void fail(int code, const std::string& msg) { throw Fail{code, msg}; }
-
-void hip_check(hipError_t e, const char* what) {
-  if (e != hipSuccess) fail(PHYAI_EHIP, std::string(what) + ": " + hipGetErrorString(e));
-}
-#define HIPC(x) hip_check((x), #x)
 
 uint16_t f2bf(float f) {
   uint32_t u;
@@ -1607,30 +1594,11 @@ int64_t pend_floats(const phyai_expert& e, int B) {
 // ---------------------------------------------------------------------------
 // C ABI
 // ---------------------------------------------------------------------------
-namespace {
-int run_guarded(const std::function<void()>& f) {
-  try {
-    f();
-    g_err.clear();
-    return PHYAI_OK;
-  } catch (const Fail& x) {
-    g_err = x.msg;
-    return x.code;
-  } catch (const std::bad_alloc&) {
-    g_err = "host allocation failed";
-    return PHYAI_ENOMEM;
-  } catch (const std::exception& x) {
-    g_err = x.what();
-    return PHYAI_EINVAL;
-  }
-}
-}  // namespace
-
 extern "C" {
 
 int phyai_version(void) { return 100; }
 
-const char* phyai_last_error(void) { return g_err.c_str(); }
+const char* phyai_last_error(void) { return last_error().c_str(); }
 
 int phyai_load_expert(const phyai_config* cfg, const phyai_tensor* tensors, int32_t n_tensors, void* stream,
                       phyai_expert** out) {
