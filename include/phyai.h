@@ -490,6 +490,31 @@ int64_t phyai_paged_attention_workspace(const phyai_paged_cache* cache, int32_t 
 int phyai_paged_gather(const phyai_paged_cache* cache, const int32_t* kv_len, void* out, int32_t rows,
                        int32_t* status, void* stream);
 
+/* phyai_prefill chunk by chunk over a paged cache (handle of variant
+ * PHYAI_VARIANT_PREFIX_LM): the keys and values of each request's next tokens, of every
+ * layer, are appended to its pages after the tokens have attended, layer by layer, to
+ * what the request has in the cache and to one another.  One chunk of a whole
+ * prefix with causal = 0 leaves, after phyai_paged_gather, what phyai_prefill computes;
+ * later chunks (text that arrives after the images, single tokens) see the earlier
+ * ones and are not seen by them.
+ *
+ *   embeds      device float32 [batch][rows][d_model]; rows at or beyond new_len[b]
+ *               are never read.
+ *   cache       n_layers, n_kv_heads and head_dim of the model; F32 on the fp32 path,
+ *               BF16 or FP8E4M3 on the bf16 path; batch <= max_batch.
+ *   past_len    host [batch]: tokens already in the cache.  new_len host [batch], 0 .. rows;
+ *               past_len + new_len <= max_pages * page_size.
+ *   rows        1 .. prefix_cap.   causal 0: the tokens of a chunk see one another; 1:
+ *               each sees those up to itself.
+ *   workspace   as for phyai_paged_attention with the model's query heads, these rows
+ *               and the largest past_len + new_len.
+ *   status      device int32 or NULL: PHYAI_PAGED_BAD_PAGE where a page number is out of
+ *               range (that request's keys and values are then NaN or missing).
+ * Work is enqueued on `stream`; calls on one handle must be ordered on the device. */
+int phyai_prefill_paged(phyai_expert* e, const float* embeds, const phyai_paged_cache* cache,
+                        const int32_t* past_len, const int32_t* new_len, int32_t rows, int32_t causal,
+                        void* workspace, int64_t workspace_bytes, int32_t* status, void* stream);
+
 /* Free every device buffer and graph of the handle.  NULL is accepted. */
 void phyai_free_expert(phyai_expert* e);
 

@@ -103,3 +103,36 @@ def paged_gather(k_pool, v_pool, table, kv_len, rows):
         for i, pool in enumerate((k_pool, v_pool)):
             out[i, b, :n] = tokens_of(pool, table[b], n).reshape(n, kd)
     return out
+
+
+def prefill_chunks(cfg, weights, x, chunks, causal):
+    """K/V of one request's tokens fed in chunks: x [n, d], chunks: (length, causal) of each.
+    A token sees every token of the chunks before its own, and of its own all (causal
+    false) or those up to itself.  Returns [L][2][n][n_kv * d_h]."""
+    from .numerics import attention, decode_stored, gelu_tanh
+    L, nq, nkv, D, n = cfg.n_layers, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, x.shape[0]
+    pos, allowed, at = np.arange(n), np.zeros((n, n), dtype=bool), 0
+    for m, up_to in zip(chunks, causal):
+        rows = slice(at, at + m)
+        allowed[rows, :at + m] = True
+        if up_to:
+            allowed[rows] &= pos[None, :] <= pos[rows, None]
+        at += m
+    out, h = np.zeros((L, 2, n, nkv * D)), np.asarray(x, dtype=np.float64)
+
+    def W(name):
+        return decode_stored(weights[name]).astype(np.float64, copy=False)
+
+    for l in range(L):
+        p = f"layers.{l}."
+        a = rms_normalize(h, cfg.rms_eps) * (1.0 + W(p + "attn_norm")[0])
+        q, k, v = ((a @ W(p + w)).reshape(n, -1, D) for w in ("wq", "wk", "wv"))
+        if cfg.rope:
+            q, k = rope(q, pos, cfg.rope_base), rope(k, pos, cfg.rope_base)
+        out[l, 0], out[l, 1] = k.reshape(n, nkv * D), v.reshape(n, nkv * D)
+        if l + 1 == L:
+            break
+        h = h + attention(q, k, v, allowed).reshape(n, nq * D) @ W(p + "wo")
+        m = rms_normalize(h, cfg.rms_eps) * (1.0 + W(p + "mlp_norm")[0])
+        h = h + (gelu_tanh(m @ W(p + "w_gate")) * (m @ W(p + "w_up"))) @ W(p + "w_down")
+    return out

@@ -24,7 +24,7 @@ _DTYPE = {"f32": 0, "bf16": 1, "fp8": 2, "fp4": 3}
 EXPORTS = ("phyai_load_expert", "phyai_denoise", "phyai_denoise_static", "phyai_prepare", "phyai_debug_hidden",
            "phyai_profile_stage", "phyai_fp8_to_bf16", "phyai_free_expert", "phyai_last_error",
            "phyai_version", "phyai_prefill", "phyai_encode_images", "phyai_qk_norm_rope", "phyai_paged_append",
-           "phyai_paged_attention", "phyai_paged_attention_workspace", "phyai_paged_gather")
+           "phyai_paged_attention", "phyai_paged_attention_workspace", "phyai_paged_gather", "phyai_prefill_paged")
 STAGES = {"norm1": 0, "qkv": 1, "attn": 2, "oproj": 3, "norm2": 4, "mlp_up": 5, "mlp_down": 6}
 
 
@@ -90,13 +90,14 @@ def lib() -> ctypes.CDLL:
         L.phyai_paged_attention.argtypes = [vp, i32, vp, vp, vp, vp, i32, f32, i32, i32, i32, i32, vp, i64, vp, vp]
         L.phyai_paged_attention_workspace.argtypes = [vp, i32, i32, i32]
         L.phyai_paged_gather.argtypes = [vp, vp, vp, i32, vp, vp]
+        L.phyai_prefill_paged.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, i64, vp, vp]
         L.phyai_free_expert.argtypes = [vp]
         L.phyai_free_expert.restype = None
         L.phyai_last_error.restype = ctypes.c_char_p
         for f in ("phyai_load_expert", "phyai_denoise", "phyai_denoise_static", "phyai_prepare", "phyai_debug_hidden",
                   "phyai_profile_stage", "phyai_fp8_to_bf16", "phyai_version", "phyai_prefill",
                   "phyai_encode_images", "phyai_qk_norm_rope", "phyai_paged_append", "phyai_paged_attention",
-                  "phyai_paged_gather"):
+                  "phyai_paged_gather", "phyai_prefill_paged"):
             getattr(L, f).restype = ctypes.c_int
         L.phyai_paged_attention_workspace.restype = i64
         _lib_handle = L
@@ -248,6 +249,32 @@ class PrefixLM:
                               device=embeds.device)
         _check(lib().phyai_prefill(self._h, _ptr(embeds), plen.ctypes.data, _ptr(out), B, _stream(stream)))
         return out
+
+    def prefill_paged(self, embeds, cache: "PagedCache", past_len, new_len=None, *, causal: bool = False,
+                      workspace=None, status=None, stream=None) -> None:
+        """Append the next tokens of each request to a paged cache of all layers
+        (``phyai_prefill_paged``).  embeds: device float32 [batch][rows][d];
+        past_len, new_len (default: rows): host arrays."""
+        import torch
+        B, rows = int(embeds.shape[0]), int(embeds.shape[1])
+        if embeds.dim() != 3 or embeds.dtype != torch.float32 or B != cache.batch or embeds.shape[2] != self.cfg.d_model:
+            raise ValueError("embeds: expected float32 [batch of the cache][rows][d_model]")
+        if embeds.device != cache.k.device:
+            raise ValueError("embeds: the device must be the cache's")
+        past = np.ascontiguousarray(past_len, dtype=np.int32)
+        new = np.full(B, rows, np.int32) if new_len is None else np.ascontiguousarray(new_len, dtype=np.int32)
+        if past.shape[0] < B or new.shape[0] < B:
+            raise ValueError("past_len or new_len shorter than the batch")
+        longest = max(1, int((past[:B].astype(np.int64) + new[:B]).max()))
+        with _Device(embeds, stream) as s:
+            if workspace is None and longest <= cache.capacity and rows > 0:
+                need = paged_attention_workspace(cache, self.cfg.n_q_heads, rows, longest)
+                if need:
+                    workspace = torch.empty(need, dtype=torch.uint8, device=embeds.device)
+            _check(lib().phyai_prefill_paged(
+                self._h, _ptr(embeds), cache._ref, past.ctypes.data, new.ctypes.data, rows, int(causal),
+                None if workspace is None else workspace.data_ptr(),
+                0 if workspace is None else workspace.numel() * workspace.element_size(), _status(status, embeds), s))
 
     def profile_stage(self, stage: str, reps: int, stream=None):
         """Enqueue `reps` passes over the layers of one block stage (timing aid;

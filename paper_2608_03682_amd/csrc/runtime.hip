@@ -20,6 +20,7 @@
 #include "../../include/phyai.h"
 #include "errors.hpp"
 #include "kernels.hpp"
+#include "paged_host.hpp"
 
 using namespace phyai;
 
@@ -126,6 +127,10 @@ struct phyai_expert {
   bool split_act = false;
   void *n_lo = nullptr, *g_lo = nullptr;
   CallDesc* desc = nullptr;
+  // prefix LM over a paged cache: projected rows [q | k | v] of every head, and the
+  // lengths before and after a chunk (descriptors of which only the lengths are used)
+  void* qkv = nullptr;
+  CallDesc *past_desc = nullptr, *kv_desc = nullptr;
   // timestep tables
   void *tau = nullptr, *c1 = nullptr, *cact = nullptr;
   float *T = nullptr, *modtab = nullptr, *adatab = nullptr, *fintab = nullptr, *dt = nullptr;
@@ -997,6 +1002,62 @@ void enqueue_prefill(phyai_expert& e, const float* embeds, void* kv_out, int B, 
   }
 }
 
+// The prefix LM over a chunk of each request's tokens, its keys and values in a paged
+// cache: embeddings into the residual stream, then per layer the norm, the projection
+// into rows [q | k | v] (every head through the query side of the epilogue, which
+// stores heads in their order), the rotation of the queries at the chunk's
+// positions, the append (keys rotated on the way), and, all but the last layer, the
+// chunk's attention over the request's cached tokens, the output projection, the MLP
+// norm and the MLP.  Rows are padded to `rows` a request; what the padding rows hold
+// reaches no other row.
+template <typename T>
+void enqueue_prefill_paged(phyai_expert& e, const float* embeds, const phyai_paged_cache* cache, int rows, int max_kv,
+                           int causal, void* workspace, int64_t workspace_bytes, int32_t* status, hipStream_t s) {
+  const int L = e.L, d = e.d, D = e.D, B = cache->batch, R = B * rows;
+  const int heads = e.nq + 2 * e.nkv, dtype = e.f32 ? PHYAI_DTYPE_F32 : PHYAI_DTYPE_BF16;
+  const float base = e.c.rope ? e.c.rope_base : 0.f;
+  T *n = static_cast<T*>(e.n), *qkv = static_cast<T*>(e.qkv), *o = static_cast<T*>(e.o), *g = static_cast<T*>(e.g);
+  const int32_t *new_len = e.desc->prefix_len, *past_len = e.past_desc->prefix_len, *kv_len = e.kv_desc->prefix_len;
+  const int64_t ld = (int64_t)heads * D;
+  const phyai_head_rows q{qkv, rows * ld, ld, D, e.nq};
+  const phyai_head_rows k{qkv + e.qd, rows * ld, ld, D, e.nkv};
+  const phyai_head_rows v{qkv + e.qd + e.kd, rows * ld, ld, D, e.nkv};
+  const phyai_head_rows out{o, (int64_t)rows * e.qd, e.qd, D, e.nq};
+  PendingResid pending{};
+  auto resid = [&](const Lin& w, const void* a, int lda) {
+    GemmArgs ga = gargs(w, a, lda, R);
+    pending = PendingResid{};
+    const int sk = e.f32 ? 1 : gemm_split_k(R, w.NPT, w.K);
+    if (sk > 1) {
+      ga.split_out = e.pend;
+      ga.split_stride = (int64_t)R * d;
+      ga.split_k = sk;
+      pending.part = e.pend;
+      pending.n = sk;
+      pending.stride = (int64_t)R * d;
+    }
+    gemm_resid(ga, EpiResid{e.h, d, nullptr, nullptr}, s);
+  };
+  prefill_embed(e.desc, embeds, e.h, B, rows, d, s);
+  for (int l = 0; l < L; ++l) {
+    const LayerW& w = e.layers[l];
+    norm_rows(e.h, n, static_cast<T*>(nullptr), R, d, e.c.rms_eps, NORM_RMS, w.attn_norm, nullptr, pending, s);
+    gemm_qkv(gargs(w.qkv, n, d, R),
+             EpiQkv<T>{qkv, nullptr, nullptr, D, heads, 0, 0, rows, 0, 0, nullptr, e.desc, nullptr}, s);
+    if (l + 1 < L && base > 0.f)
+      enqueue_norm_rope(&q, nullptr, &q, nullptr, nullptr, nullptr, 0.f, base, past_len, new_len, B, rows, D, dtype,
+                        status, s);
+    enqueue_append(cache, l, &k, &v, base, past_len, new_len, rows, dtype, status, s);
+    if (l + 1 == L) break;
+    enqueue_attention(cache, l, &q, &out, kv_len, new_len, max_kv, 1.0f / std::sqrt((float)D), causal, 0, rows, dtype,
+                      workspace, workspace_bytes, status, s);
+    resid(w.o, o, e.qd);
+    norm_rows(e.h, n, static_cast<T*>(nullptr), R, d, e.c.rms_eps, NORM_RMS, w.mlp_norm, nullptr, pending, s);
+    gemm_geglu(gargs(w.gu, n, d, R), EpiGeglu<T>{g, e.F, nullptr}, s);
+    resid(w.down, g, e.F);
+  }
+}
+
 // The vision tower over B requests (B * n_img images of M = n_patches rows):
 // patches into the GEMM operand and position embeddings into the residual
 // stream, the patch-embedding GEMM adding x W + b on top, the blocks, the
@@ -1146,6 +1207,17 @@ void load_prefix_lm(const phyai_tensor* tensors, int32_t n_tensors, hipStream_t 
           if (sk > 1) pend = std::max(pend, (int64_t)sk * R * d);
         }
     }
+  // a chunk over a paged cache has any number of rows up to max_batch * prefix_cap; the
+  // split of many rows depends on their 128-row tiles
+  if (!e->f32 && L > 1)
+    for (int64_t R = 1; R <= Bm * M; R = R < 256 ? R + 1 : std::max(R + 1, std::min(Bm * M, (R / 128 + 1) * 128)))
+      for (const Lin* w : {&e->layers[0].o, &e->layers[0].down}) {
+        const int sk = gemm_split_k(static_cast<int>(R), w->NPT, w->K);
+        if (sk > 1) pend = std::max(pend, (int64_t)sk * R * d);
+      }
+  e->qkv = e->mem.alloc(Bm * M * (e->qd + 2 * e->kd) * ab);
+  e->past_desc = static_cast<CallDesc*>(e->mem.alloc(sizeof(CallDesc)));
+  e->kv_desc = static_cast<CallDesc*>(e->mem.alloc(sizeof(CallDesc)));
   e->part = e->mem.alloc_n<float>(part > 0 ? part : 4);
   e->pend = e->mem.alloc_n<float>(pend);
   e->part_cur = e->part;
@@ -1741,6 +1813,50 @@ int phyai_prefill(phyai_expert* e, const float* embeds, const int32_t* prefix_le
     write_call_desc(*e, embeds, prefix_len, nullptr, batch, nullptr, nullptr, s);
     if (e->f32) enqueue_prefill<float>(*e, embeds, kv_out, batch, s);
     else enqueue_prefill<bf16_t>(*e, embeds, kv_out, batch, s);
+    HIPC(hipGetLastError());
+  });
+}
+
+int phyai_prefill_paged(phyai_expert* e, const float* embeds, const phyai_paged_cache* cache, const int32_t* past_len,
+                        const int32_t* new_len, int32_t rows, int32_t causal, void* workspace, int64_t workspace_bytes,
+                        int32_t* status, void* stream) {
+  return run_guarded([&] {
+    if (!e) fail(PHYAI_EINVAL, "NULL handle");
+    if (e->c.variant != PHYAI_VARIANT_PREFIX_LM) fail(PHYAI_EINVAL, "not a prefix-LM handle");
+    (void)page_pool(cache, 0);
+    const int B = cache->batch;
+    if (B > e->Bmax) fail(PHYAI_EINVAL, "the cache's batch is out of range 1..max_batch");
+    if (cache->n_layers != e->L || cache->n_kv_heads != e->nkv || cache->head_dim != e->D)
+      fail(PHYAI_EINVAL, "the cache's layers, K/V heads or head_dim are not the model's");
+    if ((cache->dtype == PHYAI_DTYPE_F32) != e->f32)
+      fail(PHYAI_EINVAL, "the cache must be F32 on the fp32 path, BF16 or FP8E4M3 on the bf16 path");
+    if (rows < 1 || rows > e->M) fail(PHYAI_EINVAL, "rows out of range 1..prefix_cap");
+    if (causal != 0 && causal != 1) fail(PHYAI_EINVAL, "causal must be 0 or 1");
+    if (!embeds || !past_len || !new_len) fail(PHYAI_EINVAL, "NULL argument");
+    if ((reinterpret_cast<uintptr_t>(embeds) & 15u) != 0) fail(PHYAI_EINVAL, "embeds must be 16-byte aligned");
+    const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
+    CallDesc hn{}, hp{}, hk{};
+    int max_kv = 1;
+    for (int b = 0; b < B; ++b) {
+      const std::string at = "[" + std::to_string(b) + "]";
+      if (new_len[b] < 0 || new_len[b] > rows) fail(PHYAI_EINVAL, "new_len" + at + " outside 0..rows");
+      if (past_len[b] < 0 || past_len[b] + (int64_t)new_len[b] > cap)
+        fail(PHYAI_EINVAL, "past_len" + at + " + new_len" + at + " outside 0..max_pages * page_size");
+      hn.prefix_len[b] = new_len[b];
+      hp.prefix_len[b] = past_len[b];
+      hk.prefix_len[b] = past_len[b] + new_len[b];
+      max_kv = std::max(max_kv, hk.prefix_len[b]);
+    }
+    const int64_t need = e->L > 1 ? attention_workspace(cache, e->nq, rows, max_kv) : 0;
+    if (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u) != 0))
+      fail(PHYAI_EINVAL, "workspace must be given and 16-byte aligned");
+    if (workspace_bytes < need) fail(PHYAI_EINVAL, "workspace too small: ask phyai_paged_attention_workspace");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    set_call_desc(hn, e->desc, s);
+    set_call_desc(hp, e->past_desc, s);
+    set_call_desc(hk, e->kv_desc, s);
+    if (e->f32) enqueue_prefill_paged<float>(*e, embeds, cache, rows, max_kv, causal, workspace, workspace_bytes, status, s);
+    else enqueue_prefill_paged<bf16_t>(*e, embeds, cache, rows, max_kv, causal, workspace, workspace_bytes, status, s);
     HIPC(hipGetLastError());
   });
 }

@@ -209,3 +209,27 @@ def test_oracle_append_then_gather():
     np.testing.assert_allclose(g[0, 0, 10:30], rope(x[0], 10 + np.arange(20), 1e4).reshape(20, 8), rtol=1e-12)
     assert (g[0, 0, :10] == pool[2, :10, 0]).all() and (g[:, :, 30:] == 0).all()
     assert (got[3] == pool[3]).all() and (got[0, 14:] == pool[0, 14:]).all()
+
+
+def test_oracle_chunks_are_the_prefix_block_and_the_causal_model():
+    """One chunk without a causal mask is the pinned prefix LM; causal chunks do not depend
+    on where they are cut; a later chunk leaves the earlier ones as they were."""
+    import oracle
+    import workloads as wl
+    cfg = wl.CONFIGS["plm_tiny_fp32"]
+    case = wl.make_prefill_case(cfg, seed=3)
+    n = 24
+    x = np.asarray(case.embeds[0, :n], dtype=np.float64)
+    one = op.prefill_chunks(cfg, case.weights, x, [n], [False])
+    np.testing.assert_allclose(one, oracle.prefill_request(cfg, case.weights, x), rtol=1e-10, atol=1e-12)
+    a = op.prefill_chunks(cfg, case.weights, x, [n], [True])
+    b = op.prefill_chunks(cfg, case.weights, x, [9, 1, 14], [True] * 3)
+    np.testing.assert_allclose(a, b, rtol=1e-10, atol=1e-12)
+    c = op.prefill_chunks(cfg, case.weights, x, [9, 15], [False, True])
+    np.testing.assert_allclose(c[:, :, :9], oracle.prefill_request(cfg, case.weights, x[:9]), rtol=1e-10, atol=1e-12)
+    assert np.abs(c - a).max() > 1e-4 and np.abs(c - one).max() > 1e-4
+
+
+def test_prefill_paged_refuses_without_a_handle():
+    assert px.lib().phyai_prefill_paged(None, P, ctypes.byref(cache()), None, None, 4, 0, None, 0, None, None) == EINVAL
+    assert b"NULL handle" in px.lib().phyai_last_error()
