@@ -81,15 +81,15 @@ __device__ __forceinline__ float pair_sum(float x) {
 // LDS tiles hold rows of RB bytes in 16-byte chunks, chunk c of row r at
 // c ^ swz(r), so that the lanes of one fragment read fall in different banks:
 //   K   16 lanes read 16 consecutive rows at one chunk
-//   V   bf16: 16 lanes read 32 bytes of each of 4 rows, the other lane half the
-//       next 4 rows; f32: 32 lanes read 128 bytes of one row, the other half of
-//       the row 4 further on
+//   V   bf16: 32 lanes, which the LDS serves at once, read 64 bytes of each of 4
+//       rows, so rows 0 .. 3 differ in the bits above those 64 bytes; f32: 32 lanes
+//       read 128 bytes of one row, the other half of the row 4 further on
 template <int RB>
 __device__ __forceinline__ int k_swz(int r) { return RB >= 256 ? (r & 15) : ((r >> 1) & 7); }
 template <int ES, int RB>
 __device__ __forceinline__ int v_swz(int r) {
   if (ES == 4) return 8 * ((r >> 2) & 1);
-  return RB >= 256 ? 2 * (r & 7) : 2 * ((r >> 1) & 3);
+  return RB >= 256 ? 4 * (r & 3) + 2 * ((r >> 2) & 1) : 4 * ((r >> 1) & 1) + 2 * ((r >> 2) & 1);
 }
 
 // Order of one MFMA loop whose operands come from LDS: PD reads ahead, then each
