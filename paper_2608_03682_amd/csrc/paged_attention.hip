@@ -127,6 +127,8 @@ struct Shape {
   static constexpr int SETS = KEYS ? NW : 1;            // tile sets
   static constexpr int LDS = SETS * 4 * TILE;           // [set][buffer][K, V]
   static constexpr int STEP = KEYS ? NW * KT : KT;      // keys of one turn of the loop
+  // rows: the scores run a tile ahead
+  static constexpr bool kAhead = !KEYS && ES == 2 && D == 256;
   // blocks of a CU that LDS and registers allow; also the waves of a SIMD asked for
   static constexpr int PER_CU = KEYS ? (LDS <= 64 * 1024 ? 2 : 1) : (LDS <= 64 * 1024 ? 2 : 1);
 };
@@ -198,7 +200,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     }
   }
 
-  // keys of the block, of this split and of this wave's rows
+  // keys of the block and of this split
   const int tok0 = (rt * ROWS) / G, tok1 = min(n - 1, (rt * ROWS + ROWS - 1) / G);
   const int bl = seen_begin(tok0, n, kv, a.window) / KT * KT, bh = seen_end(tok1, n, kv, a.causal);
   int kbeg = bl, kend = bh;
@@ -208,8 +210,6 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     kbeg = bl + split * per;
     kend = min(bh, kbeg + per);
   }
-  const int wl = seen_begin(min(wrow / G, n - 1), n, kv, a.window);
-  const int wh = wrow < rows ? seen_end(min(n - 1, (wrow + 31) / G), n, kv, a.causal) : 0;
 
   const float ks = S::kFp8 ? a.pool.k_scale[kvh] : 1.f;
   const float vs = S::kFp8 ? a.pool.v_scale[kvh] : 1.f;
@@ -237,7 +237,12 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     }
     pages = out ? 0 : id;
   };
-  auto page_of = [&](int key) { return __builtin_amdgcn_readlane(pages, (key >> a.pool.page_shift) - pbase); };
+  // where the page of a key starts, from the pool's start (page numbers are not negative
+  // here: unsigned products take half the instructions)
+  auto page_at = [&](int key) {
+    const uint32_t page = __builtin_amdgcn_readlane(pages, (key >> a.pool.page_shift) - pbase);
+    return page * static_cast<uint64_t>(a.pool.page_bytes);
+  };
 
   constexpr int GB = S::kFp8 ? D : RB;                  // bytes of a row in its page
   constexpr int LPR = GB / 16;                          // lanes of a row
@@ -254,45 +259,52 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const uint32_t kc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : k_swz<RB>(wrow0 + lrow)));
   const uint32_t vc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : v_swz<ES, RB>(wrow0 + lrow)));
   uint4 kr[S::kFp8 ? NLD : 1], vr[S::kFp8 ? NLD : 1];
-  auto issue = [&](uint32_t buf, int k0) {
-    const int lastp = min(k0 + KT - 1, kend - 1) >> a.pool.page_shift;
-    if (lastp >= pbase + kWave) load_pages(k0 >> a.pool.page_shift);
-    const bool whole = k0 + KT <= kend;
+  // The window holds the pages of keys from .. to (fewer than 64 pages), `from` and later
+  // ones being all that is still needed.
+  auto cover = [&](int from, int to) {
+    if ((min(to, kend) - 1) >> a.pool.page_shift >= pbase + kWave) load_pages(from >> a.pool.page_shift);
+  };
+  const int big_page = a.pool.page_shift >= (KT == 64 ? 6 : 5);   // a page holds whole tiles
+  const uint32_t token_bytes = a.pool.token_bytes;
+  auto load = [&](bool is_v, uint32_t buf, int i, const char* p, uint32_t row_off) {
+    const uint32_t off = row_off + (is_v ? vc ^ (S::kFp8 ? 0 : 16 * v_swz<ES, RB>(row_of(i)))
+                                         : kc ^ (S::kFp8 ? 0 : 16 * k_swz<RB>(row_of(i))));
+    if constexpr (S::kFp8) (is_v ? vr : kr)[i] = *reinterpret_cast<const uint4*>(p + off);
+    else dma16(p, off, lds0 + buf + (is_v ? 2 * TILE : 0) + (wrow0 + row_of(i)) * RB);
+  };
+  auto issue = [&](bool is_v, uint32_t buf, int k0) {
+    const char* pool = is_v ? vpool : kpool;
+    if (k0 + KT > kend) {
+      // the range ends inside the tile: lanes behind it read its last key again
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) {
-      const int r0 = wrow0 + row_of(i);
-      const int key = min(k0 + r0, kend - 1);
-      int64_t base = (int64_t)page_of(key) * a.pool.page_bytes;
-      uint32_t ro = lane_row;
-      if (whole) {
-        base += (int64_t)((k0 + r0) & psm) * a.pool.token_bytes;
-      } else {
-        // the range ends inside the tile: lanes behind it read its last key again
-        ro = static_cast<uint32_t>(min(k0 + r0 + lrow, kend - 1) & psm) * a.pool.token_bytes;
+      for (int i = 0; i < NLD; ++i) {
+        const int key = k0 + wrow0 + row_of(i);
+        load(is_v, buf, i, pool + page_at(min(key, kend - 1)),
+             static_cast<uint32_t>(min(key + lrow, kend - 1) & psm) * token_bytes);
       }
-      const uint32_t ko = ro + (kc ^ (S::kFp8 ? 0 : 16 * k_swz<RB>(row_of(i))));
-      const uint32_t vo = ro + (vc ^ (S::kFp8 ? 0 : 16 * v_swz<ES, RB>(row_of(i))));
-      if constexpr (S::kFp8) {
-        kr[i] = *reinterpret_cast<const uint4*>(kpool + base + ko);
-        vr[i] = *reinterpret_cast<const uint4*>(vpool + base + vo);
-      } else {
-        dma16(kpool + base, ko, lds0 + buf + r0 * RB);
-        dma16(vpool + base, vo, lds0 + buf + 2 * TILE + r0 * RB);
+    } else if (big_page) {
+      const char* p = pool + page_at(k0) + static_cast<uint32_t>((k0 & psm) + wrow0) * token_bytes;
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) load(is_v, buf, i, p + row_of(i) * token_bytes, lane_row);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        const int key = k0 + wrow0 + row_of(i);
+        load(is_v, buf, i, pool + page_at(key) + static_cast<uint32_t>(key & psm) * token_bytes, lane_row);
       }
     }
   };
-  // the loads of the next tile are complete and in LDS
-  auto commit = [&](uint32_t buf) {
+  // what was issued last for K or V is complete and in LDS
+  auto commit = [&](bool is_v, uint32_t buf) {
     if constexpr (S::kFp8) {
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
         const int r = wrow0 + row_of(i) + lrow, c = 2 * (lane % LPR);
-        char* kt = sm + (KEYS ? wave : 0) * 4 * TILE + buf + r * RB;
-        char* vt = kt + 2 * TILE;
-        *reinterpret_cast<bf16x8*>(kt + 16 * (c ^ k_swz<RB>(r))) = fp8x8_to_bf16x8(kr[i].x, kr[i].y);
-        *reinterpret_cast<bf16x8*>(kt + 16 * ((c + 1) ^ k_swz<RB>(r))) = fp8x8_to_bf16x8(kr[i].z, kr[i].w);
-        *reinterpret_cast<bf16x8*>(vt + 16 * (c ^ v_swz<ES, RB>(r))) = fp8x8_to_bf16x8(vr[i].x, vr[i].y);
-        *reinterpret_cast<bf16x8*>(vt + 16 * ((c + 1) ^ v_swz<ES, RB>(r))) = fp8x8_to_bf16x8(vr[i].z, vr[i].w);
+        const int sw = is_v ? v_swz<ES, RB>(r) : k_swz<RB>(r);
+        const uint4 w = (is_v ? vr : kr)[i];
+        char* row = sm + (KEYS ? wave : 0) * 4 * TILE + buf + (is_v ? 2 * TILE : 0) + r * RB;
+        *reinterpret_cast<bf16x8*>(row + 16 * (c ^ sw)) = fp8x8_to_bf16x8(w.x, w.y);
+        *reinterpret_cast<bf16x8*>(row + 16 * ((c + 1) ^ sw)) = fp8x8_to_bf16x8(w.z, w.w);
       }
     } else {
       dma_wait();
@@ -332,9 +344,9 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     return lds_at<float>((at ^ (128u * db)) + (32 * kb + 8 * (v / 4) + v % 4) * RB);
   };
 
-  auto compute = [&](uint32_t buf, int k0) {
-    const uint32_t ka = k_at ^ buf, tv = v_at ^ buf;
-    f32x16 st[KB];
+  // S^T of one tile
+  auto scores = [&](f32x16 (&st)[KB], uint32_t buf) {
+    const uint32_t ka = k_at ^ buf;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -354,18 +366,9 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
           st[kb] = mfma_f32(__uint_as_float(kf.w), __uint_as_float(qf[s].w), st[kb]);
         }
       }
-    if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
-    // hidden keys get -inf, only in tiles where a row of the wave has any
-    const bool need_mask = __ballot(k0 < lo || k0 + KT > hi) != 0;
-    if (need_mask) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int key = k0 + 32 * kb + 8 * (v / 4) + 4 * hl + v % 4;
-          st[kb][v] = key >= lo && key < hi ? st[kb][v] : -INFINITY;
-        }
-    }
+  };
+  // this lane's largest score (its half of the tile's keys)
+  auto half_max = [&](const f32x16 (&st)[KB]) {
     float mx[2 * KB];
 #pragma unroll
     for (int c = 0; c < 2 * KB; ++c) {
@@ -376,12 +379,26 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       m = max3(m, x[f + 5], x[f + 6]);
       mx[c] = max2(m, x[f + 7]);
     }
-    float tmax = max2(mx[0], mx[1]);
-    if constexpr (KB == 2) tmax = max3(tmax, mx[2], mx[3]);
-    tmax = pair_max(tmax) * sl2;
-    // The reference m moves only when a tile's maximum exceeds it by more than 8
-    // (powers of two: p stays below 2^8), so the accumulators are rescaled a few
-    // times per key range and not at every tile.
+    if constexpr (KB == 2) return max3(max2(mx[0], mx[1]), mx[2], mx[3]);
+    else return max2(mx[0], mx[1]);
+  };
+  // hidden keys get -inf, only in tiles where a row of the wave has any
+  auto hide = [&](f32x16 (&st)[KB], float& tmax, int k0) {
+    if (__ballot(k0 < lo || k0 + KT > hi) == 0) return;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int key = k0 + 32 * kb + 8 * (v / 4) + 4 * hl + v % 4;
+        st[kb][v] = key >= lo && key < hi ? st[kb][v] : -INFINITY;
+      }
+    tmax = half_max(st);
+  };
+  // The reference m moves only when a tile's maximum exceeds it by more than 8
+  // (powers of two: p stays below 2^8), so the accumulators are rescaled a few
+  // times per key range and not at every tile.
+  auto rescale = [&](float half) {
+    const float tmax = pair_max(half) * sl2;
     if (__ballot(tmax > m_run + 8.f)) {
       const float m_new = fmaxf(m_run, tmax);
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
@@ -390,9 +407,11 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       for (int i = 0; i < D / 32; ++i) o[i] *= alpha;
       m_run = m_new;
     }
+  };
+  // P^T of one tile as the B operand, and its sum into l
+  auto weights = [&](f32x16 (&st)[KB], bf16x8 (&pf)[2 * KB]) {
     const float m_use = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every p is 0
     float ps[2 * KB];
-    bf16x8 pf[2 * KB];
 #pragma unroll
     for (int t = 0; t < 2 * KB; ++t) {
       float pv[8];
@@ -413,12 +432,15 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     }
     if constexpr (KB == 2) l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
     else l_run += ps[0] + ps[1];
+  };
+  // O^T += V^T P^T
+  auto values = [&](const f32x16 (&st)[KB], const bf16x8 (&pf)[2 * KB], uint32_t buf) {
+    const uint32_t tv = v_at ^ buf;
     if constexpr (ES == 2) {
 #pragma unroll
       for (int t = 0; t < 2 * KB; ++t)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) o[db] = mfma32x32x16(v_bf16(tv, t, db), pf[t], o[db]);
-      mfma_pipeline<2 * KB * (D / 32), 2, 2>();
     } else {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -429,26 +451,170 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     }
   };
 
+  // Scores of the next tile and values of this one, written out in the order in which
+  // they are to issue, one product after another: N1 of K Q^T, then N2 of V^T P^T, each
+  // with the LDS reads of the product PD further on and its share of the exponentials.
+  // The P of a group of 16 keys is ready when the first product that takes it comes.
+  // Left to itself the compiler puts the N1 products first and all vector work beside
+  // the N2 (head_dim 128, 4,096 rows over 8,192 keys: 485 us).
+  auto scores_and_values = [&](f32x16 (&next)[KB], const f32x16 (&st)[KB], uint32_t buf) {
+    constexpr int DB = D / 32, N1 = KB * NQ, N2 = 2 * KB * DB, N = N1 + N2, NE = 16 * KB, SPAN = N - DB, PD = 4;
+    const uint32_t ka = k_at ^ buf ^ TILE, tv = v_at ^ buf;
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    bf16x8 frag[PD], pf[2 * KB];
+    float pv[8], ps[2 * KB];
+    auto read = [&](int i) {
+      if (i < N1) {
+        const u32x4 w = lds_at<u32x4>((ka ^ (32u * (i / KB))) + 32 * (i % KB) * RB);
+        frag[i % PD] = __builtin_bit_cast(bf16x8, w);
+      } else if (i < N) {
+        frag[i % PD] = v_bf16(tv, (i - N1) / DB, (i - N1) % DB);
+      }
+    };
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) next[kb][v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < PD; ++i) read(i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < N1) next[i % KB] = mfma32x32x16(frag[i % PD], as_bf16x8(qf[i / KB]), next[i % KB]);
+      else o[(i - N1) % DB] = mfma32x32x16(frag[i % PD], pf[(i - N1) / DB], o[(i - N1) % DB]);
+      read(i + PD);
+      const int e0 = i * NE / SPAN, e1 = (i + 1) * NE / SPAN;
+#pragma unroll
+      for (int e = e0; e < e1 && e < NE; ++e) {
+        const int t = e / 8, j = e % 8;
+        pv[j] = __builtin_amdgcn_exp2f(fmaf(st[t >> 1][8 * (t & 1) + j], sl2, -m_use));
+        if (j == 7) {
+          ps[t] = ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
+          pf[t] = as_bf16x8(make_uint4(pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
+                                       pack_bf16x2(pv[6], pv[7])));
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (KB == 2) l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+    else l_run += ps[0] + ps[1];
+  };
+
   // ---- the key range ----
-  int k0 = kbeg + (KEYS ? wave * KT : 0);
-  if (k0 < kend) {
+  if constexpr (KEYS) {
+    int k0 = kbeg + wave * KT;
+    if (k0 < kend) {
+      // two buffers: the next tile is under way while this one is worked on
+      uint32_t buf = 0;
+      load_pages(k0 >> a.pool.page_shift);
+      issue(false, 0, k0);
+      issue(true, 0, k0);
+      commit(false, 0);
+      commit(true, 0);
+      for (;;) {
+        const int next = k0 + S::STEP;
+        const bool more = next < kend;
+        if (more) {
+          cover(next, next + KT);
+          issue(false, buf ^ TILE, next);
+          issue(true, buf ^ TILE, next);
+        }
+        f32x16 st[KB];
+        bf16x8 pf[2 * KB];
+        scores(st, buf);
+        if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
+        float half = half_max(st);
+        hide(st, half, k0);
+        rescale(half);
+        weights(st, pf);
+        values(st, pf, buf);
+        if constexpr (ES == 2) mfma_pipeline<2 * KB * (D / 32), 2, 2>();
+        if (!more) break;
+        commit(false, buf ^ TILE);
+        commit(true, buf ^ TILE);
+        k0 = next;
+        buf ^= TILE;
+      }
+    }
+  } else if (!S::kAhead && kbeg < kend) {
     // two buffers: the next tile is under way while this one is worked on
     uint32_t buf = 0;
-    load_pages(k0 >> a.pool.page_shift);
-    issue(0, k0);
-    commit(0);
-    if constexpr (!KEYS) lds_barrier();
-    for (;;) {
-      const int next = k0 + S::STEP;
-      const bool more = next < kend;
-      if (more) issue(buf ^ TILE, next);
-      if (KEYS || (k0 < wh && k0 + KT > wl)) compute(buf, k0);
-      if (more) commit(buf ^ TILE);
-      if constexpr (!KEYS) lds_barrier();
+    load_pages(kbeg >> a.pool.page_shift);
+    issue(false, 0, kbeg);
+    issue(true, 0, kbeg);
+    commit(false, 0);
+    commit(true, 0);
+    lds_barrier();
+    for (int k0 = kbeg;; k0 += KT, buf ^= TILE) {
+      const bool more = k0 + KT < kend;
+      if (more) {
+        cover(k0 + KT, k0 + 2 * KT);
+        issue(false, buf ^ TILE, k0 + KT);
+        issue(true, buf ^ TILE, k0 + KT);
+      }
+      f32x16 st[KB];
+      bf16x8 pf[2 * KB];
+      scores(st, buf);
+      if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
+      float half = half_max(st);
+      hide(st, half, k0);
+      rescale(half);
+      weights(st, pf);
+      values(st, pf, buf);
+      if constexpr (ES == 2) mfma_pipeline<2 * KB * (D / 32), 2, 2>();
       if (!more) break;
-      k0 = next;
-      buf ^= TILE;
+      commit(false, buf ^ TILE);
+      commit(true, buf ^ TILE);
+      lds_barrier();
     }
+  } else if (S::kAhead && kbeg < kend) {
+    // The scores of tile t + 1 are computed beside the exponentials of tile t, so that
+    // the matrix cores work while the vector units do: K runs a tile ahead of V.
+    // K(t) and V(t) lie in buffer t % 2; step t reads K(t + 1) and V(t) and loads
+    // K(t + 2) and V(t + 1), whose buffers the step before was the last to read.
+    f32x16 st[KB];
+    bf16x8 pf[2 * KB];
+    load_pages(kbeg >> a.pool.page_shift);
+    issue(false, 0, kbeg);
+    issue(true, 0, kbeg);
+    commit(false, 0);
+    commit(true, 0);
+    if (kbeg + KT < kend) {
+      issue(false, TILE, kbeg + KT);
+      commit(false, TILE);
+    }
+    lds_barrier();
+    scores(st, 0);
+    float half = half_max(st);
+    hide(st, half, kbeg);
+    lds_barrier();
+    uint32_t buf = 0;
+    int k0 = kbeg;
+    for (; k0 + KT < kend; k0 += KT, buf ^= TILE) {
+      const bool more = k0 + 2 * KT < kend;
+      cover(k0 + KT, k0 + 3 * KT);
+      if (more) issue(false, buf, k0 + 2 * KT);
+      issue(true, buf ^ TILE, k0 + KT);
+      rescale(half);
+      f32x16 next[KB];
+      if constexpr (ES == 2) {
+        scores_and_values(next, st, buf);
+      } else {
+        scores(next, buf ^ TILE);
+        weights(st, pf);
+        values(st, pf, buf);
+      }
+      half = half_max(next);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) st[kb] = next[kb];
+      hide(st, half, k0 + KT);
+      if (more) commit(false, buf);
+      commit(true, buf ^ TILE);
+      lds_barrier();
+    }
+    rescale(half);
+    weights(st, pf);
+    values(st, pf, buf);
   }
   l_run = pair_sum(l_run);
 
