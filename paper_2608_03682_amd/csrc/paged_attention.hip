@@ -16,9 +16,9 @@
 // Two shapes of block:
 //   rows   NW waves x 32 query rows, K/V tiles shared by the waves: chunks, which
 //          are bound by the matrix cores and the exponentials;
-//   keys   every wave works on the same 32 rows and on key tiles of its own,
-//          joined in LDS at the end: few rows, which are bound by reading K/V.
-// Either may split the keys over blocks as well; a second kernel joins the splits.
+//   keys   one wave on 32 rows, one tile of K and of V in LDS, many waves a CU: few
+//          rows, which are bound by reading K/V.
+// Either may split the keys over blocks; a second kernel joins the splits.
 #include "common.hpp"
 #include "errors.hpp"
 #include "paged.hpp"
@@ -111,6 +111,16 @@ __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
 }
 
+// The 18 wait states between a 32-bit product and the first reader of its result.  The
+// compiler counts them too, but not where the reader is the copy out of an accumulator
+// register that opens the block after a branch (two 32-bit kernels read the last of
+// sixteen scores 4 states after the product).
+__device__ __forceinline__ void mfma_settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // What a block of one kind looks like.  CT: element of the pool, T: of the rows
 // and of the products.
 template <typename CT, typename T, int D, bool KEYS>
@@ -121,28 +131,27 @@ struct Shape {
   static constexpr int CPR = RB / 16;                   // chunks of a row
   static constexpr int KT = (ES == 2 && !KEYS) ? 64 : 32;   // keys of a tile
   static constexpr int TILE = KT * RB;                  // bytes of a K or V tile
-  // keys: as many waves as 128 KiB of double-buffered tiles allow, at most 4
-  static constexpr int NW = KEYS ? (4 * TILE * 4 <= 128 * 1024 ? 4 : (4 * TILE * 2 <= 128 * 1024 ? 2 : 1)) : 4;
-  static constexpr int ROWS = KEYS ? 32 : 32 * NW;      // query rows of a block
-  static constexpr int SETS = KEYS ? NW : 1;            // tile sets
-  static constexpr int LDS = SETS * 4 * TILE;           // [set][buffer][K, V]
-  static constexpr int STEP = KEYS ? NW * KT : KT;      // keys of one turn of the loop
+  static constexpr int NW = KEYS ? 1 : 4;
+  static constexpr int ROWS = 32 * NW;                  // query rows of a block
+  static constexpr int BUFS = KEYS ? 1 : 2;             // buffers of K and of V
+  static constexpr int LDS = 2 * BUFS * TILE;
   // rows: the scores run a tile ahead
   static constexpr bool kAhead = !KEYS && ES == 2 && D == 256;
-  // blocks of a CU that LDS and registers allow; also the waves of a SIMD asked for
-  static constexpr int PER_CU = KEYS ? (LDS <= 64 * 1024 ? 2 : 1) : (LDS <= 64 * 1024 ? 2 : 1);
+  // waves of a SIMD asked for, and with them blocks of a CU
+  static constexpr int PER_SIMD = KEYS ? (RB <= 128 ? 4 : RB <= 256 ? 2 : 1) : (LDS <= 64 * 1024 ? 2 : 1);
+  static constexpr int LDS_BLOCKS = 160 * 1024 / LDS;
+  static constexpr int PER_CU = LDS_BLOCKS < 4 * PER_SIMD / NW ? LDS_BLOCKS : 4 * PER_SIMD / NW;
 };
 
 template <typename CT, typename T, int D, bool KEYS, int NT = 64 * Shape<CT, T, D, KEYS>::NW,
-          int PER_SIMD = Shape<CT, T, D, KEYS>::PER_CU>
+          int PER_SIMD = Shape<CT, T, D, KEYS>::PER_SIMD>
 __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs a) {
   using S = Shape<CT, T, D, KEYS>;
   constexpr int ES = S::ES, RB = S::RB, CPR = S::CPR, KT = S::KT, KB = KT / 32, TILE = S::TILE, NW = S::NW;
+  constexpr int V_AT = S::BUFS * TILE;                  // LDS: [K, V][buffer][TILE]
   constexpr int ROWS = S::ROWS, NQ = RB / 32;           // chunk pairs of a row
   // aligned so that the two buffers of a tile differ in one address bit
   __shared__ __attribute__((aligned(2 * TILE))) char sm[S::LDS];
-  __shared__ float s_ml[NW][32][2];
-  __shared__ uint32_t s_nan;
   __shared__ int s_bad;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -174,15 +183,14 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const int n = span.n, rows = n * G;
   if (rt * ROWS >= rows) return;
 
-  if (threadIdx.x == 0) {
-    s_nan = 0;
-    s_bad = 0;
+  if constexpr (!KEYS) {
+    if (threadIdx.x == 0) s_bad = 0;
+    __syncthreads();
   }
-  __syncthreads();
 
   // this lane's query row and the keys it sees; a lane behind the last row works on
   // zeros and sees what the others see
-  const int wrow = rt * ROWS + (KEYS ? 0 : wave * 32);
+  const int wrow = rt * ROWS + wave * 32;
   const int row = wrow + lr;
   const bool valid = row < rows;
   const int tok = valid ? row / G : n - 1;
@@ -205,8 +213,8 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const int bl = seen_begin(tok0, n, kv, a.window) / KT * KT, bh = seen_end(tok1, n, kv, a.causal);
   int kbeg = bl, kend = bh;
   if (a.n_split > 1) {
-    const int steps = bh > bl ? (bh - bl + S::STEP - 1) / S::STEP : 0;
-    const int per = (steps + a.n_split - 1) / a.n_split * S::STEP;
+    const int steps = bh > bl ? (bh - bl + KT - 1) / KT : 0;
+    const int per = (steps + a.n_split - 1) / a.n_split * KT;
     kbeg = bl + split * per;
     kend = min(bh, kbeg + per);
   }
@@ -216,8 +224,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const float sl2 = fmaxf(a.scale * ks * kLog2e, 1e-37f);  // not 0: a hidden key's -inf stays -inf
 
   // ---- loading ----
-  // LDS: [set][K, V][buffer][TILE]; addresses of the two buffers differ in one bit
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)sm)) + (KEYS ? wave : 0) * 4 * TILE;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)sm));
   const int psm = (1 << a.pool.page_shift) - 1;
   const int32_t* table = a.pool.table + (int64_t)b * a.pool.table_stride;
   const char* kpool = a.pool.k + kvh * a.pool.head_bytes;
@@ -247,14 +254,14 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   constexpr int GB = S::kFp8 ? D : RB;                  // bytes of a row in its page
   constexpr int LPR = GB / 16;                          // lanes of a row
   constexpr int RPI = kWave / LPR;                      // rows of one load instruction
-  constexpr int NLD = KT / RPI / (KEYS ? 1 : NW);       // load instructions of a wave, per operand
-  static_assert(KT % RPI == 0 && (KEYS || KT / RPI % NW == 0) && NLD >= 1, "whole loads");
+  constexpr int NLD = KT / RPI / NW;                    // load instructions of a wave, per operand
+  static_assert(KT % RPI == 0 && KT / RPI % NW == 0 && NLD >= 1, "whole loads");
   static_assert(RPI <= 16, "the rows of one load lie in one page");
   // Row first_row(i) + lane / LPR, chunk lane % LPR.  A lane's place in its row is
   // chunk ^ swizzle; what of the swizzle depends on i is a constant, since
   // first_row(i) and lane / LPR share no bits.
-  const int lrow = lane / LPR, wrow0 = (KEYS ? 0 : wave) * RPI;
-  auto row_of = [&](int i) { return (KEYS ? i : NW * i) * RPI; };   // first_row(i) - wrow0
+  const int lrow = lane / LPR, wrow0 = wave * RPI;
+  auto row_of = [&](int i) { return NW * i * RPI; };   // first_row(i) - wrow0
   const uint32_t lane_row = static_cast<uint32_t>(lrow) * a.pool.token_bytes;
   const uint32_t kc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : k_swz<RB>(wrow0 + lrow)));
   const uint32_t vc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : v_swz<ES, RB>(wrow0 + lrow)));
@@ -270,7 +277,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     const uint32_t off = row_off + (is_v ? vc ^ (S::kFp8 ? 0 : 16 * v_swz<ES, RB>(row_of(i)))
                                          : kc ^ (S::kFp8 ? 0 : 16 * k_swz<RB>(row_of(i))));
     if constexpr (S::kFp8) (is_v ? vr : kr)[i] = *reinterpret_cast<const uint4*>(p + off);
-    else dma16(p, off, lds0 + buf + (is_v ? 2 * TILE : 0) + (wrow0 + row_of(i)) * RB);
+    else dma16(p, off, lds0 + buf + (is_v ? V_AT : 0) + (wrow0 + row_of(i)) * RB);
   };
   auto issue = [&](bool is_v, uint32_t buf, int k0) {
     const char* pool = is_v ? vpool : kpool;
@@ -302,17 +309,13 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
         const int r = wrow0 + row_of(i) + lrow, c = 2 * (lane % LPR);
         const int sw = is_v ? v_swz<ES, RB>(r) : k_swz<RB>(r);
         const uint4 w = (is_v ? vr : kr)[i];
-        char* row = sm + (KEYS ? wave : 0) * 4 * TILE + buf + (is_v ? 2 * TILE : 0) + r * RB;
+        char* row = sm + buf + (is_v ? V_AT : 0) + r * RB;
         *reinterpret_cast<bf16x8*>(row + 16 * (c ^ sw)) = fp8x8_to_bf16x8(w.x, w.y);
         *reinterpret_cast<bf16x8*>(row + 16 * ((c + 1) ^ sw)) = fp8x8_to_bf16x8(w.z, w.w);
       }
     } else {
       dma_wait();
     }
-    // keys: other lanes of this wave read what was written here; LDS operations of a
-    // wave complete in order, the compiler has to keep that order.  rows: the
-    // barrier publishes the tile and tells that everybody is done with the other.
-    if constexpr (KEYS) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
 
   // ---- one tile ----
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const int i16 = lane % 16, vr0 = ES == 2 ? 4 * hl + i16 / 4 : 4 * hl;
   const uint32_t k_at = lds0 + lr * RB + 16 * (hl ^ k_swz<RB>(lr));
   const uint32_t v_at =
-      lds0 + 2 * TILE + vr0 * RB +
+      lds0 + V_AT + vr0 * RB +
       (ES == 2 ? 16 * ((2 * ((lane / 16) % 2) + (i16 % 4) / 2) ^ v_swz<ES, RB>(vr0)) + 8 * (i16 & 1)
                : 16 * ((lr / 4) ^ v_swz<ES, RB>(vr0)) + 4 * (lr % 4));
   auto v_bf16 = [&](uint32_t at, int t, int db) {
@@ -366,6 +369,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
           st[kb] = mfma_f32(__uint_as_float(kf.w), __uint_as_float(qf[s].w), st[kb]);
         }
       }
+    if constexpr (ES == 4) mfma_settle();
   };
   // this lane's largest score (its half of the tile's keys)
   auto half_max = [&](const f32x16 (&st)[KB]) {
@@ -502,38 +506,45 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
 
   // ---- the key range ----
   if constexpr (KEYS) {
-    int k0 = kbeg + wave * KT;
-    if (k0 < kend) {
-      // two buffers: the next tile is under way while this one is worked on
-      uint32_t buf = 0;
-      load_pages(k0 >> a.pool.page_shift);
-      issue(false, 0, k0);
-      issue(true, 0, k0);
-      commit(false, 0);
-      commit(true, 0);
-      for (;;) {
-        const int next = k0 + S::STEP;
-        const bool more = next < kend;
-        if (more) {
-          cover(next, next + KT);
-          issue(false, buf ^ TILE, next);
-          issue(true, buf ^ TILE, next);
-        }
+    // One buffer each: K's is refilled once the scores are computed, V's once the values
+    // are, so a wave has most of a tile in flight at any time, and many waves fit a CU.
+    if (kbeg < kend) {
+      auto wait = [&](bool last) {                      // all loads but the youngest tile's
+        if (last) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(S::kFp8 ? 63 : NLD) : "memory");
+      };
+      // other lanes read what a lane wrote, and loads overwrite what lanes have read: LDS
+      // operations of a wave complete in order, the compiler has to keep that order
+      auto fence = [&] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+      load_pages(kbeg >> a.pool.page_shift);
+      issue(false, 0, kbeg);
+      issue(true, 0, kbeg);
+      if constexpr (S::kFp8) commit(false, 0);
+      wait(false);
+      for (int k0 = kbeg;; k0 += KT) {
+        const bool more = k0 + KT < kend;
         f32x16 st[KB];
         bf16x8 pf[2 * KB];
-        scores(st, buf);
+        scores(st, 0);
         if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
+        fence();
+        if (more) {
+          cover(k0 + KT, k0 + 2 * KT);
+          issue(false, 0, k0 + KT);
+        }
         float half = half_max(st);
         hide(st, half, k0);
         rescale(half);
         weights(st, pf);
-        values(st, pf, buf);
+        if constexpr (S::kFp8) commit(true, 0);
+        wait(!more);
+        values(st, pf, 0);
         if constexpr (ES == 2) mfma_pipeline<2 * KB * (D / 32), 2, 2>();
         if (!more) break;
-        commit(false, buf ^ TILE);
-        commit(true, buf ^ TILE);
-        k0 = next;
-        buf ^= TILE;
+        fence();
+        issue(true, 0, k0 + KT);
+        if constexpr (S::kFp8) commit(false, 0);
+        wait(false);
       }
     }
   } else if (!S::kAhead && kbeg < kend) {
@@ -668,77 +679,16 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
 
   // ---- out ----
   // an unusable page or length makes the block's rows NaN
-  if (bad && lane == 0) s_bad = 1;
-  __syncthreads();
-  bad = __builtin_amdgcn_readfirstlane(s_bad) != 0;
+  if constexpr (!KEYS) {
+    if (bad && lane == 0) s_bad = 1;
+    __syncthreads();
+    bad = __builtin_amdgcn_readfirstlane(s_bad) != 0;
+  }
   if (bad) {
     m_run = 0.f;
     l_run = __builtin_nanf("");
   }
-  if constexpr (KEYS) {
-    // the waves' parts, chunk c of row r at c ^ (r % 16)
-    float* so = reinterpret_cast<float*>(sm) + wave * 32 * D;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int c = 8 * db + 2 * u + hl;
-        *reinterpret_cast<float4*>(so + lr * D + 4 * (c ^ (lr & 15))) =
-            make_float4(o[db][4 * u], o[db][4 * u + 1], o[db][4 * u + 2], o[db][4 * u + 3]);
-      }
-    if (hl == 0) {
-      s_ml[wave][lr][0] = m_run;
-      s_ml[wave][lr][1] = l_run;
-    }
-    if (nan_rows && lane == 0) atomicOr(&s_nan, nan_rows);
-    __syncthreads();
-    const int live = min(32, rows - wrow);
-    for (int x = threadIdx.x; x < live * (D / 4); x += 64 * NW) {
-      const int r = x / (D / 4), c = x % (D / 4);
-      float mm = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) mm = fmaxf(mm, s_ml[w][r][0]);
-      float l = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float lw = s_ml[w][r][1];
-        const float f = lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_ml[w][r][0] - mm);
-        if (lw != 0.f) {
-          const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<float*>(sm) + (w * 32 + r) * D +
-                                                            4 * (c ^ (r & 15)));
-          acc.x = fmaf(f, v.x, acc.x);
-          acc.y = fmaf(f, v.y, acc.y);
-          acc.z = fmaf(f, v.z, acc.z);
-          acc.w = fmaf(f, v.w, acc.w);
-          l = fmaf(f, lw, l);
-        }
-      }
-      const int rr = wrow + r;
-      if (a.n_split == 1) {
-        const float inv = l == 0.f ? 0.f : vs / l;
-        const float v4[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
-        T* op = static_cast<T*>(a.out.p) + b * a.out.b + (rr / G) * a.out.t + (kvh * G + rr % G) * a.out.h + 4 * c;
-        ActIO<T>::store4(op, v4);
-      } else {
-        const int64_t at = (grow + rr) * a.n_split + split;
-        *reinterpret_cast<float4*>(a.part + at * D + 4 * c) = acc;
-        if (c == 0) a.ml[at] = make_float2(mm, l);
-      }
-    }
-    const uint32_t redo = __builtin_amdgcn_readfirstlane(s_nan);
-    if (redo && !bad) {
-      __syncthreads();                                  // the rows above are written
-      for (int r = wave; r < 32; r += NW) {
-        if (!(redo >> r & 1)) continue;
-        float mm = -INFINITY, l = 0.f;
-        for (int w = 0; w < NW; ++w) mm = fmaxf(mm, s_ml[w][r][0]);
-        for (int w = 0; w < NW; ++w)
-          if (s_ml[w][r][1] != 0.f) l = fmaf(__builtin_amdgcn_exp2f(s_ml[w][r][0] - mm), s_ml[w][r][1], l);
-        repair(wrow + r, mm, l);
-      }
-    }
-  } else if (a.n_split > 1) {
+  if (a.n_split > 1) {
     if (valid) {
       const int64_t at = (grow + row) * a.n_split + split;
 #pragma unroll
@@ -777,14 +727,12 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       }
     }
   }
-  if constexpr (!KEYS) {
-    if (nan_rows && !bad) {
-      dma_wait();                                       // the rows above are written
-      for (uint32_t left = nan_rows; left; left &= left - 1) {
-        const int r = __builtin_ctz(left);
-        repair(wrow + r, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m_run), r)),
-               __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_run), r)));
-      }
+  if (nan_rows && !bad) {
+    dma_wait();                                         // the rows above are written
+    for (uint32_t left = nan_rows; left; left &= left - 1) {
+      const int r = __builtin_ctz(left);
+      repair(wrow + r, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m_run), r)),
+             __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_run), r)));
     }
   }
 }
@@ -819,12 +767,22 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, bool f
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   const float* part = a.part + gr * a.n_split * D + E * lane;
-  for (int s = 0; s < a.n_split; ++s) {
-    const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
-    const float lsp = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l), s));
-    if (lsp == 0.f) continue;
+  // eight splits under way at once; those past the last and those without a key are
+  // read (the workspace has them) and not taken
+  for (int s0 = 0; s0 < a.n_split; s0 += 8) {
+    float v[8][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(ws, part[(int64_t)s * D + e], acc[e]);
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = part[(int64_t)min(s0 + k, a.n_split - 1) * D + e];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (s0 + k >= a.n_split) break;
+      const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s0 + k));
+      const float ls = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l), s0 + k));
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(ws, ls == 0.f ? 0.f : v[k][e], acc[e]);
+    }
   }
   const float inv = total == 0.f ? 0.f : (fp8 ? a.pool.v_scale[kvh] : 1.f) / total;
   T* op = static_cast<T*>(a.out.p) + b * a.out.b + (row / a.G) * a.out.t + (kvh * a.G + row % a.G) * a.out.h + E * lane;
@@ -859,7 +817,7 @@ void plan(PagedAttnArgs& a) {
   a.n_tiles = (a.M * a.G + S::ROWS - 1) / S::ROWS;
   const int64_t base = (int64_t)a.B * a.nkv * a.n_tiles;
   const int64_t slots = 256 * S::PER_CU;
-  const int steps = std::max(1, (a.max_kv + S::STEP - 1) / S::STEP);
+  const int steps = std::max(1, (a.max_kv + S::KT - 1) / S::KT);
   // A block costs its steps plus about one to start and one to finish, a launch the
   // rounds of its blocks over the chip, joining about two steps.
   int best = 1;
