@@ -121,7 +121,7 @@ struct PagedAttnArgs {
   int32_t* status;
   float* part;              // n_split > 1: [B][nkv][M * G][n_split][D], not normalised
   float2* ml;               // and each split's (maximum, sum): [B][nkv][M * G][n_split]
-  int B, M, nkv, G, max_kv, causal, window, n_split, n_tiles;
+  int B, M, nkv, G, max_kv, causal, window, n_split, split_keys, n_tiles;
   float scale;
 };
 
@@ -131,8 +131,9 @@ enum PagedKind { PAGED_F32 = 0, PAGED_BF16 = 1, PAGED_FP8 = 2 };
 void norm_rope(const NormRopeArgs& a, int D, int kind, hipStream_t s);
 void paged_append(const PagedAppendArgs& a, int D, int row_kind, int pool_kind, hipStream_t s);
 void paged_gather(const PagedGatherArgs& a, int pool_kind, hipStream_t s);
-// Plans the launch (row tiles, key splits) for a.B, M, nkv, G and max_kv, then floats
-// of workspace it needs; paged_attention launches what was planned.
+// Plans the launch (row tiles, key splits) for a.B, M, nkv, G, max_kv and window and
+// gives the floats of workspace it needs, most without a window; paged_attention
+// launches what was planned.
 int64_t paged_attention_plan(PagedAttnArgs& a, int D, int pool_kind);
 void paged_attention(const PagedAttnArgs& a, int D, int pool_kind, hipStream_t s);
 

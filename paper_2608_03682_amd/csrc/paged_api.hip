@@ -178,7 +178,8 @@ void enqueue_append(const phyai_paged_cache* cache, int layer, const phyai_head_
 namespace {
 
 // What the size and place of the split depend on.
-PagedAttnArgs attention_plan(const phyai_paged_cache* cache, int n_q_heads, int rows, int max_kv_len, int64_t& floats) {
+PagedAttnArgs attention_plan(const phyai_paged_cache* cache, int n_q_heads, int rows, int max_kv_len, int window,
+                             int64_t& floats) {
   check_sizes(cache->batch, rows, cache->head_dim);
   req(n_q_heads >= 1 && n_q_heads <= kMaxHeads && n_q_heads % cache->n_kv_heads == 0,
       "query heads must be a multiple of n_kv_heads, at most 1024");
@@ -190,6 +191,7 @@ PagedAttnArgs attention_plan(const phyai_paged_cache* cache, int n_q_heads, int 
   a.nkv = cache->n_kv_heads;
   a.G = n_q_heads / cache->n_kv_heads;
   a.max_kv = max_kv_len;
+  a.window = window;
   req((int64_t)a.B * n_q_heads * rows <= INT32_MAX / 2, "batch * rows * query heads out of range");
   floats = paged_attention_plan(a, cache->head_dim, pool_kind(cache));
   return a;
@@ -200,7 +202,7 @@ PagedAttnArgs attention_plan(const phyai_paged_cache* cache, int n_q_heads, int 
 int64_t attention_workspace(const phyai_paged_cache* cache, int n_q_heads, int rows, int max_kv_len) {
   (void)page_pool(cache, 0);
   int64_t floats = 0;
-  attention_plan(cache, n_q_heads, rows, max_kv_len, floats);
+  attention_plan(cache, n_q_heads, rows, max_kv_len, 0, floats);
   return floats * 4;
 }
 
@@ -215,12 +217,12 @@ void enqueue_attention(const phyai_paged_cache* cache, int layer, const phyai_he
   const HeadRows hq = head_rows(q, dtype, "q");
   const HeadRows ho = out_rows(out, dtype, "out", cache->batch, rows, cache->head_dim);
   req(hq.n == ho.n, "out has another number of heads than q");
-  int64_t floats = 0;
-  PagedAttnArgs a = attention_plan(cache, hq.n, rows, max_kv_len, floats);
   req(kv_len, "kv_len must not be NULL");
   req(std::isfinite(scale) && scale > 0.f, "scale must be a positive number");
   req(causal == 0 || causal == 1, "causal must be 0 or 1");
   req(window >= 0 && (window == 0 || causal), "window must be >= 0, and 0 without a causal mask");
+  int64_t floats = 0;
+  PagedAttnArgs a = attention_plan(cache, hq.n, rows, max_kv_len, window, floats);
   req(floats == 0 || (workspace && aligned16(workspace)), "workspace must be given and 16-byte aligned");
   req(workspace_bytes >= floats * 4, "workspace too small: ask phyai_paged_attention_workspace");
   a.pool = pool;
@@ -230,7 +232,6 @@ void enqueue_attention(const phyai_paged_cache* cache, int layer, const phyai_he
   a.new_len = new_len;
   a.status = status;
   a.causal = causal;
-  a.window = window;
   a.scale = scale;
   a.part = static_cast<float*>(workspace);
   a.ml = reinterpret_cast<float2*>(a.part + floats / (cache->head_dim + 2) * cache->head_dim);

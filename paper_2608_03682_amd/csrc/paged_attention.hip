@@ -197,6 +197,22 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const int qhead = kvh * G + (valid ? row % G : 0);
   const int hi = seen_end(tok, n, kv, a.causal), lo = seen_begin(tok, n, kv, a.window);
 
+  // keys of the block and of this split
+  const int tok0 = (rt * ROWS) / G, tok1 = min(n - 1, (rt * ROWS + ROWS - 1) / G);
+  const int bl = seen_begin(tok0, n, kv, a.window) / KT * KT, bh = seen_end(tok1, n, kv, a.causal);
+  int kbeg = bl, kend = bh;
+  if (a.n_split > 1) {
+    kbeg = bl + split * a.split_keys;
+    kend = min(bh, kbeg + a.split_keys);
+  }
+
+  const int64_t grow = (int64_t)grp * a.M * G;          // first row of (request, K/V head) in the workspace
+  if (a.n_split > 1 && kbeg >= kend && !bad) {
+    // no key of this split is seen: a weight of 0, which the join does not follow
+    if (valid && hl == 0) a.ml[(grow + row) * a.n_split + split] = make_float2(-INFINITY, 0.f);
+    return;
+  }
+
   // Q^T operand: chunk 2 s + h of the row
   uint4 qf[NQ];
   {
@@ -206,17 +222,6 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       qf[s] = make_uint4(0, 0, 0, 0);
       if (valid) qf[s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
     }
-  }
-
-  // keys of the block and of this split
-  const int tok0 = (rt * ROWS) / G, tok1 = min(n - 1, (rt * ROWS + ROWS - 1) / G);
-  const int bl = seen_begin(tok0, n, kv, a.window) / KT * KT, bh = seen_end(tok1, n, kv, a.causal);
-  int kbeg = bl, kend = bh;
-  if (a.n_split > 1) {
-    const int steps = bh > bl ? (bh - bl + KT - 1) / KT : 0;
-    const int per = (steps + a.n_split - 1) / a.n_split * KT;
-    kbeg = bl + split * per;
-    kend = min(bh, kbeg + per);
   }
 
   const float ks = S::kFp8 ? a.pool.k_scale[kvh] : 1.f;
@@ -639,7 +644,6 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     for (int v = 0; v < 16; ++v) nan += o[i][v];
   const uint64_t nan_lanes = __ballot(valid && nan != nan && l_run == l_run);
   const uint32_t nan_rows = static_cast<uint32_t>(nan_lanes) | static_cast<uint32_t>(nan_lanes >> 32);
-  const int64_t grow = (int64_t)grp * a.M * G;          // first row of (request, K/V head) in the workspace
   auto repair = [&](int rr, float m, float l) {
     constexpr int E = D / kWave;
     const int t = rr / G;
@@ -737,39 +741,37 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   }
 }
 
-// Joins the splits of one row per wave: o = sum_s w_s o_s / sum_s w_s l_s, w_s =
-// 2^(m_s - max m), in the order of the splits.  Splits without a key have l = 0
-// and are not read.
-template <typename T, int D>
+// Joins the splits of a row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max m).
+// W waves take the splits of a row in turn, eight loads under way each, and add up in
+// LDS in a fixed order.  Splits without a key have l = 0 and are not taken.
+template <typename T, int D, int W>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, bool fp8) {
   constexpr int E = D / kWave;
+  __shared__ float part_sum[W > 1 ? W : 1][D];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int MG = a.M * a.G;
-  const int64_t gr = (int64_t)blockIdx.x * 4 + wave;
+  const int MG = a.M * a.G, wr = wave % W;
+  const int64_t gr = (int64_t)blockIdx.x * (4 / W) + wave / W;
   if (gr >= (int64_t)a.B * a.nkv * MG) return;
   const int grp = static_cast<int>(gr / MG), row = static_cast<int>(gr % MG);
   const int b = grp / a.nkv, kvh = grp % a.nkv;
+  // requested together: every split's (m, l), and the length
+  float2 x = make_float2(-INFINITY, 0.f);
+  if (lane < a.n_split) x = a.ml[gr * a.n_split + lane];
   const RowSpan span = row_span(a.new_len ? a.new_len[b] : a.M, 0, a.M, a.M);
   if (row >= span.n * a.G) return;
-  const float2* ml = a.ml + gr * a.n_split;
-  float m = -INFINITY, l = 0.f;
-  if (lane < a.n_split) {
-    const float2 x = ml[lane];
-    m = x.x;
-    l = x.y;
-  }
-  float mm = m;
+  const float l = x.y;
+  float mm = l == 0.f ? -INFINITY : x.x;
 #pragma unroll
   for (int s = 1; s < kWave; s <<= 1) mm = fmaxf(mm, __shfl_xor(mm, s, kWave));
-  const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - mm);
+  const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(x.x - mm);
   const float total = wave_sum(l == 0.f ? 0.f : w * l);
+  const uint64_t live = __ballot(l != 0.f);
   float acc[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   const float* part = a.part + gr * a.n_split * D + E * lane;
-  // eight splits under way at once; those past the last and those without a key are
-  // read (the workspace has them) and not taken
-  for (int s0 = 0; s0 < a.n_split; s0 += 8) {
+  for (int s0 = 8 * wr; s0 < a.n_split; s0 += 8 * W) {
+    if ((live >> s0 & 0xff) == 0) continue;
     float v[8][E];
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -777,11 +779,22 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, bool f
       for (int e = 0; e < E; ++e) v[k][e] = part[(int64_t)min(s0 + k, a.n_split - 1) * D + e];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      if (s0 + k >= a.n_split) break;
-      const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s0 + k));
-      const float ls = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l), s0 + k));
+      const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), (s0 + k) & 63));
+      const bool take = s0 + k < a.n_split && (live >> (s0 + k) & 1);
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(ws, ls == 0.f ? 0.f : v[k][e], acc[e]);
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(ws, take ? v[k][e] : 0.f, acc[e]);
+    }
+  }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) part_sum[wr][E * lane + e] = acc[e];
+    __syncthreads();
+    if (wr > 0) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      acc[e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < W; ++k) acc[e] += part_sum[k][E * lane + e];
     }
   }
   const float inv = total == 0.f ? 0.f : (fp8 ? a.pool.v_scale[kvh] : 1.f) / total;
@@ -801,7 +814,8 @@ void launch(const PagedAttnArgs& a, hipStream_t s) {
   paged_attn_kernel<CT, T, D, KEYS><<<grid, 64 * Shape<CT, T, D, KEYS>::NW, 0, s>>>(a);
   if (a.n_split > 1) {
     const int64_t rows = (int64_t)a.B * a.nkv * a.M * a.G;
-    paged_join_kernel<T, D><<<static_cast<int>((rows + 3) / 4), 256, 0, s>>>(a, sizeof(CT) == 1);
+    if (a.n_split <= 8) paged_join_kernel<T, D, 1><<<static_cast<int>((rows + 3) / 4), 256, 0, s>>>(a, sizeof(CT) == 1);
+    else paged_join_kernel<T, D, 4><<<static_cast<int>(rows), 256, 0, s>>>(a, sizeof(CT) == 1);
   }
 }
 
@@ -817,22 +831,36 @@ void plan(PagedAttnArgs& a) {
   a.n_tiles = (a.M * a.G + S::ROWS - 1) / S::ROWS;
   const int64_t base = (int64_t)a.B * a.nkv * a.n_tiles;
   const int64_t slots = 256 * S::PER_CU;
-  const int steps = std::max(1, (a.max_kv + S::KT - 1) / S::KT);
-  // A block costs its steps plus about one to start and one to finish, a launch the
-  // rounds of its blocks over the chip, joining about two steps.
-  int best = 1;
-  int64_t least = INT64_MAX;
-  for (int n = 1; n <= std::min(64, steps); ++n) {
-    const int per = (steps + n - 1) / n;
-    if ((steps + per - 1) / per != n) continue;         // the last splits would be empty
-    const int64_t cost = (base * n + slots - 1) / slots * (per + 2) + (n > 1 ? 2 : 0);
-    if (cost < least) {
-      least = cost;
-      best = n;
+  // Splits are of equal length, so that a launch over ragged requests is made of equal
+  // blocks.  One costs its tiles plus about two to start and finish; a launch costs its
+  // blocks over the chip, at least a whole round of them and half a round at the end;
+  // joining costs about two tiles.
+  auto choose = [&](int steps, int most) {
+    int best = 1;
+    double least = 1e300;
+    for (int n = 1; n <= std::min(most, steps); ++n) {
+      const int per = (steps + n - 1) / n;
+      if ((steps + per - 1) / per != n) continue;       // the last splits would be empty
+      const double rounds = static_cast<double>(base) * n / slots;
+      const double cost = (rounds <= 1 ? 1 : rounds + 0.5) * (per + 2) + (n > 1 ? 2 : 0);
+      if (cost < least) {
+        least = cost;
+        best = n;
+      }
+      if (base * n >= 4 * slots) break;
     }
-    if (base * n >= 4 * slots) break;
+    return best;
+  };
+  // the longest range of a block; the workspace is sized without the window
+  const int steps = std::max(1, (a.max_kv + S::KT - 1) / S::KT);
+  a.n_split = choose(steps, 64);
+  int span = steps;
+  if (a.window > 0) {
+    const int64_t keys = (int64_t)a.window + (S::ROWS - 1) / a.G + 1;
+    span = static_cast<int>(std::min<int64_t>(steps, (keys + S::KT - 1) / S::KT + 1));
+    a.n_split = choose(span, a.n_split);
   }
-  a.n_split = best;
+  a.split_keys = (span + a.n_split - 1) / a.n_split * S::KT;
 }
 
 template <typename CT, typename T, int D>
