@@ -265,16 +265,19 @@ class PrefixLM:
         new = np.full(B, rows, np.int32) if new_len is None else np.ascontiguousarray(new_len, dtype=np.int32)
         if past.shape[0] < B or new.shape[0] < B:
             raise ValueError("past_len or new_len shorter than the batch")
+        if _elsewhere(embeds, stream):
+            with _there(embeds, stream):
+                return self.prefill_paged(embeds, cache, past, new, causal=causal, workspace=workspace, status=status)
         longest = max(1, int((past[:B].astype(np.int64) + new[:B]).max()))
-        with _Device(embeds, stream) as s:
-            if workspace is None and longest <= cache.capacity and rows > 0:
-                need = paged_attention_workspace(cache, self.cfg.n_q_heads, rows, longest)
-                if need:
-                    workspace = torch.empty(need, dtype=torch.uint8, device=embeds.device)
-            _check(lib().phyai_prefill_paged(
-                self._h, _ptr(embeds), cache._ref, past.ctypes.data, new.ctypes.data, rows, int(causal),
-                None if workspace is None else workspace.data_ptr(),
-                0 if workspace is None else workspace.numel() * workspace.element_size(), _status(status, embeds), s))
+        if workspace is None and longest <= cache.capacity and rows > 0:
+            need = paged_attention_workspace(cache, self.cfg.n_q_heads, rows, longest)
+            if need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=embeds.device)
+        _check(lib().phyai_prefill_paged(
+            self._h, _ptr(embeds), cache._ref, past.ctypes.data, new.ctypes.data, rows, int(causal),
+            None if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.numel() * workspace.element_size(),
+            _vector(status, torch.int32, 1, embeds, "status"), _here(embeds)))
 
     def profile_stage(self, stage: str, reps: int, stream=None):
         """Enqueue `reps` passes over the layers of one block stage (timing aid;
@@ -343,10 +346,15 @@ class VisionTower:
 # ---------------------------------------------------------------------------
 # the paged key/value cache
 # ---------------------------------------------------------------------------
+_KINDS: Dict[object, int] = {}
+
+
 def _dtype_of(t) -> int:
     """F32, BF16 (or its bit patterns as int16) and FP8E4M3 (or its codes as uint8)."""
-    import torch
-    d = {torch.float32: 0, torch.bfloat16: 1, torch.int16: 1, torch.float8_e4m3fn: 2, torch.uint8: 2}.get(t.dtype)
+    if not _KINDS:
+        import torch
+        _KINDS.update({torch.float32: 0, torch.bfloat16: 1, torch.int16: 1, torch.float8_e4m3fn: 2, torch.uint8: 2})
+    d = _KINDS.get(t.dtype)
     if d is None:
         raise ValueError(f"unsupported dtype {t.dtype}")
     return d
@@ -354,72 +362,59 @@ def _dtype_of(t) -> int:
 
 def _head_rows(t, what: str, like=None) -> _HeadRows:
     """[batch][rows][heads][head_dim] with any strides of the first three dimensions."""
-    if t.dim() != 4 or not t.is_cuda:
-        raise ValueError(f"{what}: expected a device tensor [batch][rows][heads][head_dim]")
     n, s = t.shape, t.stride()
+    if len(n) != 4 or not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor [batch][rows][heads][head_dim]")
     if s[3] != 1:
         raise ValueError(f"{what}: a head's values must be contiguous")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device or n[0] != like.shape[0] or
-                             n[1] != like.shape[1] or n[3] != like.shape[3]):
-        raise ValueError(f"{what}: batch, rows, head_dim, dtype and device must be those of the other rows")
+    if like is not None:
+        m = like.shape
+        if t.dtype != like.dtype or t.device != like.device or n[0] != m[0] or n[1] != m[1] or n[3] != m[3]:
+            raise ValueError(f"{what}: batch, rows, head_dim, dtype and device must be those of the other rows")
     # the stride of a dimension of one is nobody's
     return _HeadRows(t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0, n[2])
 
 
-def _lengths(t, batch: int, like, what: str) -> Optional[int]:
-    import torch
+def _vector(t, dtype, least: int, like, what: str) -> Optional[int]:
+    """The address of a contiguous vector of at least `least` values on the call's device."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.dim() != 1 or t.device != like.device or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous int32 tensor on {like.device}")
-    if t.shape[0] < batch:
-        raise ValueError(f"{what}: shorter than the batch")
+    if t.dtype != dtype or t.dim() != 1 or t.device != like.device or t.shape[0] < least or not t.is_contiguous():
+        raise ValueError(f"{what}: expected {least} contiguous values of {dtype} on {like.device}")
     return t.data_ptr()
 
 
-def _floats(t, n: int, like, what: str) -> Optional[int]:
+def _elsewhere(t, stream) -> bool:
+    """Whether a call has to make its device or stream the current one first."""
     import torch
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.device != like.device or not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"{what}: expected {n} contiguous float32 values on {like.device}")
-    return t.data_ptr()
+    return stream is not None or t.get_device() != torch._C._cuda_getDevice()
 
 
-def _status(t, like) -> Optional[int]:
-    import torch
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or t.device != like.device or t.numel() < 1:
-        raise ValueError(f"status: expected an int32 tensor on {like.device}")
-    return t.data_ptr()
-
-
-class _Device:
-    """The device of a call's tensors is current, and its outputs and workspace belong
-    to the call's stream, while the call is made.  The stream that is already
-    current needs neither."""
+class _there:
+    """Makes the device of a call's tensors and its stream current, so that outputs and
+    workspaces belong to them."""
 
     def __init__(self, t, stream):
         import torch
-        self._guards = []
-        self._dev = t.device
-        if t.device.index != torch.cuda.current_device():
-            self._guards.append(torch.cuda.device(t.device))
-        if stream is not None:
-            if stream.device != t.device:
-                raise ValueError(f"the stream belongs to {stream.device}, the tensors to {t.device}")
-            self._guards.append(torch.cuda.stream(stream))
+        if not t.is_cuda:
+            raise ValueError("expected a device tensor")
+        if stream is not None and stream.device != t.device:
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors to {t.device}")
+        self._device, self._stream = torch.cuda.device(t.device), torch.cuda.stream(stream)
 
-    def __enter__(self) -> int:
-        import torch
-        for g in self._guards:
-            g.__enter__()
-        return torch.cuda.current_stream(self._dev).cuda_stream
+    def __enter__(self):
+        self._device.__enter__()
+        self._stream.__enter__()
 
     def __exit__(self, *exc):
-        for g in reversed(self._guards):
-            g.__exit__(*exc)
+        self._stream.__exit__(*exc)
+        self._device.__exit__(*exc)
+
+
+def _here(t) -> int:
+    """The current stream of the tensor's device."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 class PagedCache:
@@ -451,7 +446,8 @@ class PagedCache:
         self.batch, self.page_size, self.n_kv_heads, self.head_dim = page_table.shape[0], n[1], n[2], n[3]
         width = page_table.shape[1]
         self._c = _PagedCache(
-            k.data_ptr(), v.data_ptr(), _floats(k_scale, n[2], k, "k_scale"), _floats(v_scale, n[2], k, "v_scale"),
+            k.data_ptr(), v.data_ptr(), _vector(k_scale, torch.float32, n[2], k, "k_scale"),
+            _vector(v_scale, torch.float32, n[2], k, "v_scale"),
             page_table.data_ptr(), k.stride(0) if self.n_layers > 1 else 0, s[0] if n[0] > 1 else 0, s[1],
             s[2] if n[2] > 1 else 0, dtype, self.n_layers, n[2], n[3], n[1], n[0], self.batch, width,
             page_table.stride(0) if self.batch > 1 else width)
@@ -471,29 +467,39 @@ def qk_norm_rope(q, k=None, q_gain=None, k_gain=None, *, eps: float = 1e-6, rope
     rotates, rope_base = 0 only normalises.  Returns (q_out, k_out), new tensors
     where none are given (their rows behind new_len are not written)."""
     import torch
+    if _elsewhere(q, stream):
+        with _there(q, stream):
+            return qk_norm_rope(q, k, q_gain, k_gain, eps=eps, rope_base=rope_base, past_len=past_len, new_len=new_len,
+                                q_out=q_out, k_out=k_out, status=status)
     qs = _head_rows(q, "q")
-    ks = None if k is None else _head_rows(k, "k", q)
     B, M, _, D = q.shape
-    with _Device(q, stream) as s:
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        elif q_out.shape != q.shape:
-            raise ValueError("q_out: another shape than q")
-        if k is None:
-            if k_out is not None:
-                raise ValueError("k_out without k")
-        elif k_out is None:
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif q_out.shape != q.shape:
+        raise ValueError("q_out: another shape than q")
+    qo = _head_rows(q_out, "q_out", q)
+    ks = ko = None
+    if k is not None:
+        k_struct = _head_rows(k, "k", q)
+        if k_out is None:
             k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
         elif k_out.shape != k.shape:
             raise ValueError("k_out: another shape than k")
-        qo = _head_rows(q_out, "q_out", q)
-        ko = None if k is None else _head_rows(k_out, "k_out", q)
-        if B * M > 0:
-            _check(lib().phyai_qk_norm_rope(
-                ctypes.byref(qs), None if k is None else ctypes.byref(ks), ctypes.byref(qo),
-                None if k is None else ctypes.byref(ko), _floats(q_gain, D, q, "q_gain"),
-                _floats(k_gain, D, q, "k_gain"), eps, rope_base, _lengths(past_len, B, q, "past_len"),
-                _lengths(new_len, B, q, "new_len"), B, M, D, _dtype_of(q), _status(status, q), s))
+        ko_struct = _head_rows(k_out, "k_out", q)
+        ks, ko = ctypes.byref(k_struct), ctypes.byref(ko_struct)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    for g, what in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+        if g is not None and g.shape != (D,):
+            raise ValueError(f"{what}: expected [head_dim]")
+    if B * M > 0:
+        rc = lib().phyai_qk_norm_rope(
+            ctypes.byref(qs), ks, ctypes.byref(qo), ko, _vector(q_gain, torch.float32, D, q, "q_gain"),
+            _vector(k_gain, torch.float32, D, q, "k_gain"), eps, rope_base,
+            _vector(past_len, torch.int32, B, q, "past_len"), _vector(new_len, torch.int32, B, q, "new_len"), B, M, D,
+            _dtype_of(q), _vector(status, torch.int32, 1, q, "status"), _here(q))
+        if rc:
+            _check(rc)
     return q_out, k_out
 
 
@@ -502,16 +508,22 @@ def paged_append(cache: PagedCache, k, v, past_len, *, new_len=None, rope_base: 
     """Append keys and values [batch][rows][n_kv_heads][head_dim] of new tokens to the
     cache at tokens past_len[b] .. past_len[b] + new_len[b] - 1, the keys rotated to
     those positions where rope_base is not 0 (``phyai_paged_append``)."""
+    import torch
+    if _elsewhere(k, stream):
+        with _there(k, stream):
+            return paged_append(cache, k, v, past_len, new_len=new_len, rope_base=rope_base, layer=layer, status=status)
     ks, vs = _head_rows(k, "k"), _head_rows(v, "v", k)
     B, M, _, D = k.shape
     if B != cache.batch or D != cache.head_dim or k.device != cache.k.device:
         raise ValueError("k: batch, head_dim and device must be the cache's")
     if B * M == 0:
         return
-    with _Device(k, stream) as s:
-        _check(lib().phyai_paged_append(cache._ref, layer, ctypes.byref(ks), ctypes.byref(vs), rope_base,
-                                        _lengths(past_len, B, k, "past_len"), _lengths(new_len, B, k, "new_len"), M,
-                                        _dtype_of(k), _status(status, k), s))
+    rc = lib().phyai_paged_append(cache._ref, layer, ctypes.byref(ks), ctypes.byref(vs), rope_base,
+                                  _vector(past_len, torch.int32, B, k, "past_len"),
+                                  _vector(new_len, torch.int32, B, k, "new_len"), M, _dtype_of(k),
+                                  _vector(status, torch.int32, 1, k, "status"), _here(k))
+    if rc:
+        _check(rc)
 
 
 def paged_attention_workspace(cache: PagedCache, n_q_heads: int, rows: int, max_kv_len: Optional[int] = None) -> int:
@@ -533,31 +545,38 @@ def paged_attention(q, cache: PagedCache, kv_len, *, new_len=None, max_kv_len: O
     device tensor of at least ``paged_attention_workspace`` bytes (default: one is
     allocated for the call).  Returns out (rows behind new_len are not written)."""
     import torch
+    if _elsewhere(q, stream):
+        with _there(q, stream):
+            return paged_attention(q, cache, kv_len, new_len=new_len, max_kv_len=max_kv_len, scale=scale, causal=causal,
+                                   window=window, layer=layer, out=out, workspace=workspace, status=status)
     qs = _head_rows(q, "q")
     B, M, H, D = q.shape
     if B != cache.batch or D != cache.head_dim or q.device != cache.k.device:
         raise ValueError("q: batch, head_dim and device must be the cache's")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out: another shape than q")
+    os_ = _head_rows(out, "out", q)
+    if B * M == 0:
+        return out
     if max_kv_len is None:
         max_kv_len = cache.capacity
-    with _Device(q, stream) as s:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        elif out.shape != q.shape:
-            raise ValueError("out: another shape than q")
-        if B * M == 0:
-            return out
-        os_ = _head_rows(out, "out", q)
-        need = paged_attention_workspace(cache, H, M, max_kv_len)
-        if workspace is None:
-            if need:
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        elif workspace.device != q.device or not workspace.is_contiguous():
+    if workspace is None:
+        size = paged_attention_workspace(cache, H, M, max_kv_len)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    else:
+        if workspace.device != q.device or not workspace.is_contiguous():
             raise ValueError(f"workspace: expected a contiguous tensor on {q.device}")
-        _check(lib().phyai_paged_attention(
-            cache._ref, layer, ctypes.byref(qs), ctypes.byref(os_), _lengths(kv_len, B, q, "kv_len"),
-            _lengths(new_len, B, q, "new_len"), max_kv_len, D ** -0.5 if scale is None else scale, int(causal), window,
-            M, _dtype_of(q), None if workspace is None else workspace.data_ptr(),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), _status(status, q), s))
+        size = workspace.numel() * workspace.element_size()
+    rc = lib().phyai_paged_attention(
+        cache._ref, layer, ctypes.byref(qs), ctypes.byref(os_), _vector(kv_len, torch.int32, B, q, "kv_len"),
+        _vector(new_len, torch.int32, B, q, "new_len"), max_kv_len, D ** -0.5 if scale is None else scale, causal,
+        window, M, _dtype_of(q), None if workspace is None else workspace.data_ptr(), size,
+        _vector(status, torch.int32, 1, q, "status"), _here(q))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -566,17 +585,22 @@ def paged_gather(cache: PagedCache, kv_len, rows: int, *, out=None, status=None,
     [layers][2][batch][rows][n_kv_heads * head_dim] that ``Expert.denoise`` reads
     (``phyai_paged_gather``): float32 or bfloat16, zeros behind kv_len[b]."""
     import torch
-    dt = torch.float32 if cache.k.dtype == torch.float32 else torch.bfloat16
+    k = cache.k
+    if _elsewhere(k, stream):
+        with _there(k, stream):
+            return paged_gather(cache, kv_len, rows, out=out, status=status)
+    dt = torch.float32 if k.dtype == torch.float32 else torch.bfloat16
     shape = (cache.n_layers, 2, cache.batch, rows, cache.n_kv_heads * cache.head_dim)
-    with _Device(cache.k, stream) as s:
-        if out is None:
-            out = torch.empty(shape, dtype=dt, device=cache.k.device)
-        elif tuple(out.shape) != shape or out.dtype not in (dt, torch.int16 if dt == torch.bfloat16 else dt) or \
-                not out.is_contiguous() or out.device != cache.k.device:
-            raise ValueError(f"out: expected a contiguous {dt} tensor {shape} on {cache.k.device}")
-        if cache.batch * rows > 0:
-            _check(lib().phyai_paged_gather(cache._ref, _lengths(kv_len, cache.batch, cache.k, "kv_len"),
-                                            out.data_ptr(), rows, _status(status, cache.k), s))
+    if out is None:
+        out = torch.empty(shape, dtype=dt, device=k.device)
+    elif out.shape != shape or (out.dtype != dt and (dt == torch.float32 or out.dtype != torch.int16)) or \
+            not out.is_contiguous() or out.device != k.device:
+        raise ValueError(f"out: expected a contiguous {dt} tensor {shape} on {k.device}")
+    if cache.batch * rows > 0:
+        rc = lib().phyai_paged_gather(cache._ref, _vector(kv_len, torch.int32, cache.batch, k, "kv_len"),
+                                      out.data_ptr(), rows, _vector(status, torch.int32, 1, k, "status"), _here(k))
+        if rc:
+            _check(rc)
     return out
 
 

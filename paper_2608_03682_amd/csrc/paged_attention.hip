@@ -24,6 +24,7 @@
 #include "paged.hpp"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace phyai {
@@ -832,9 +833,14 @@ void plan(PagedAttnArgs& a) {
   const int64_t base = (int64_t)a.B * a.nkv * a.n_tiles;
   const int64_t slots = 256 * S::PER_CU;
   // Splits are of equal length, so that a launch over ragged requests is made of equal
-  // blocks.  One costs its tiles plus about two to start and finish; a launch costs its
-  // blocks over the chip, at least a whole round of them and half a round at the end;
-  // joining costs about two tiles.
+  // blocks.  A block costs its tiles plus two or three to start and finish, joining two.
+  //   rows: bound by the blocks' own work, a launch costs whole rounds of blocks over the
+  //     chip (4,096 rows over 8,192 keys, two rounds unsplit: 432 us, two splits 498; 64
+  //     rows of eight requests: 86 us unsplit, 64, 66, 60, 76 with 2, 3, 4, 8 splits).
+  //   keys: bound by memory, of which a few waves a CU are enough; what costs is the half
+  //     round in which some blocks have ended, and of ragged requests many have nothing
+  //     to do (64 tokens over 600 .. 4,000 keys: 195 us unsplit, 148 with one round of
+  //     four splits, 132 .. 139 with 5 to 24; all of 2,300 keys: 120 unsplit, 128 .. 138).
   auto choose = [&](int steps, int most) {
     int best = 1;
     double least = 1e300;
@@ -842,7 +848,7 @@ void plan(PagedAttnArgs& a) {
       const int per = (steps + n - 1) / n;
       if ((steps + per - 1) / per != n) continue;       // the last splits would be empty
       const double rounds = static_cast<double>(base) * n / slots;
-      const double cost = (rounds <= 1 ? 1 : rounds + 0.5) * (per + 2) + (n > 1 ? 2 : 0);
+      const double cost = (KEYS ? (std::max(1.0, rounds) + 0.5) * (per + 3) : std::ceil(rounds) * (per + 2)) + (n > 1 ? 2 : 0);
       if (cost < least) {
         least = cost;
         best = n;
