@@ -2,6 +2,7 @@
 // then one launch (attention: two where the keys are split over blocks).
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "errors.hpp"
 #include "paged.hpp"
@@ -16,6 +17,10 @@ namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 void req(bool ok, const char* m) {
   if (!ok) fail(PHYAI_EINVAL, m);
+}
+// Lengths, scales and the status word; the status takes atomics, which fault elsewhere.
+void words(std::initializer_list<const void*> ps) {
+  for (const void* p : ps) req((reinterpret_cast<uintptr_t>(p) & 3u) == 0, "lengths, scales and status must be 4-byte aligned");
 }
 int elem_bytes(int dtype) { return dtype == PHYAI_DTYPE_F32 ? 4 : (dtype == PHYAI_DTYPE_BF16 ? 2 : 1); }
 
@@ -76,7 +81,7 @@ PagePool page_pool(const phyai_paged_cache* c, int layer) {
       "cache dtype must be F32, BF16 or FP8E4M3");
   req(c->k && c->v && c->page_table, "cache pools and page table must not be NULL");
   req(aligned16(c->k) && aligned16(c->v), "cache pools must be 16-byte aligned");
-  req((reinterpret_cast<uintptr_t>(c->page_table) & 3u) == 0, "page_table must be 4-byte aligned");
+  words({c->page_table, c->k_scale, c->v_scale});
   req(c->dtype != PHYAI_DTYPE_FP8E4M3 || (c->k_scale && c->v_scale), "an FP8E4M3 cache needs k_scale and v_scale");
   req(c->n_layers >= 1 && c->n_layers <= kMaxLayers, "cache n_layers out of range 1..1024");
   req(c->n_kv_heads >= 1 && c->n_kv_heads <= kMaxHeads, "cache n_kv_heads out of range 1..1024");
@@ -140,6 +145,7 @@ void enqueue_norm_rope(const phyai_head_rows* q, const phyai_head_rows* k, const
   req((q || !q_gain) && (k || !k_gain), "a gain without its rows");
   a.rope = rope_freq(rope_base, head_dim, a.freq);
   a.norm = eps > 0.f;
+  words({past_len, new_len, status});
   req(a.norm || a.rope, "eps and rope_base are both 0: nothing to do");
   a.q_gain = q_gain;
   a.k_gain = k_gain;
@@ -165,6 +171,7 @@ void enqueue_append(const phyai_paged_cache* cache, int layer, const phyai_head_
   a.v = head_rows(v, dtype, "v");
   req(a.k.n == cache->n_kv_heads && a.v.n == cache->n_kv_heads, "k and v must have the cache's n_kv_heads heads");
   req(past_len, "past_len must not be NULL");
+  words({past_len, new_len, status});
   a.rope = rope_freq(rope_base, cache->head_dim, a.freq);
   a.past_len = past_len;
   a.new_len = new_len;
@@ -218,6 +225,7 @@ void enqueue_attention(const phyai_paged_cache* cache, int layer, const phyai_he
   const HeadRows ho = out_rows(out, dtype, "out", cache->batch, rows, cache->head_dim);
   req(hq.n == ho.n, "out has another number of heads than q");
   req(kv_len, "kv_len must not be NULL");
+  words({kv_len, new_len, status});
   req(std::isfinite(scale) && scale > 0.f, "scale must be a positive number");
   req(causal == 0 || causal == 1, "causal must be 0 or 1");
   req(window >= 0 && (window == 0 || causal), "window must be >= 0, and 0 without a causal mask");
@@ -287,6 +295,7 @@ int phyai_paged_gather(const phyai_paged_cache* cache, const int32_t* kv_len, vo
     check_sizes(cache->batch, rows, cache->head_dim);
     req(kv_len && out, "kv_len and out must not be NULL");
     req(aligned16(out), "out must be 16-byte aligned");
+    words({kv_len, status});
     req((int64_t)cache->n_layers * 2 * cache->batch <= 65535, "n_layers * 2 * batch out of range 1..65535");
     a.kv_len = kv_len;
     a.out = out;

@@ -635,9 +635,10 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   }
   l_run = pair_sum(l_run);
 
-  // A hidden key's weight is 0, and 0 times an infinite or NaN value is NaN: rows that
-  // came out NaN although their weights are numbers are computed once more, over the
-  // keys that they see and no other, with the maximum m and sum l found above.
+  // A hidden key's weight is 0, and 0 times an infinite or NaN value is NaN: where a row
+  // came out NaN although its weights are numbers, and a key that it does not see but
+  // its block does holds such a value, it is computed once more over the keys that it
+  // sees and no other, with the maximum m and sum l found above.
   float nan = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
@@ -646,9 +647,28 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const uint64_t nan_lanes = __ballot(valid && nan != nan && l_run == l_run);
   const uint32_t nan_rows = static_cast<uint32_t>(nan_lanes) | static_cast<uint32_t>(nan_lanes >> 32);
   auto repair = [&](int rr, float m, float l) {
-    constexpr int E = D / kWave;
+    constexpr int E = D / kWave, U = 8;
     const int t = rr / G;
     const int64_t head = kvh * G + rr % G;
+    auto elem = [](const char* p, int e) {
+      if constexpr (S::kFp8) return __uint_as_float(fp8x2_to_bf16x2<false>(reinterpret_cast<const uint8_t*>(p)[e]) << 16);
+      else return ActIO<T>::load(reinterpret_cast<const T*>(p) + e);
+    };
+    // this lane's part of a key's row; the pages were checked when they were loaded
+    auto row_at = [&](int key) {
+      const int id = table[key >> a.pool.page_shift];
+      return page_row_offset(a.pool, page_ok(id, a.pool.n_pages) ? id : 0, key, kvh) + (int64_t)E * lane * sizeof(CT);
+    };
+    const int first = max(kbeg, seen_begin(t, n, kv, a.window)), end = min(kend, seen_end(t, n, kv, a.causal));
+    bool hidden = false;                                // at most a tile and the block's rows on either side
+    for (int key = kbeg; key < kend; ++key) {
+      if (key == first && first < end) key = end;
+      if (key >= kend) break;
+      const int64_t at = row_at(key);
+#pragma unroll
+      for (int e = 0; e < E; ++e) hidden |= !(fabsf(elem(a.pool.v + at, e)) < INFINITY);
+    }
+    if (__ballot(hidden) == 0) return;
     const T* qp = static_cast<const T*>(a.q.p) + b * a.q.b + t * a.q.t + head * a.q.h + E * lane;
     float q[E], acc[E];
 #pragma unroll
@@ -656,26 +676,29 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       q[e] = ActIO<T>::load(qp + e);
       acc[e] = 0.f;
     }
-    auto elem = [](const char* p, int e) {
-      if constexpr (S::kFp8) return __uint_as_float(fp8x2_to_bf16x2<false>(reinterpret_cast<const uint8_t*>(p)[e]) << 16);
-      else return ActIO<T>::load(reinterpret_cast<const T*>(p) + e);
-    };
-    const int end = min(kend, seen_end(t, n, kv, a.causal));
-    for (int key = max(kbeg, seen_begin(t, n, kv, a.window)); key < end; ++key) {
-      const int id = table[key >> a.pool.page_shift];
-      if (!page_ok(id, a.pool.n_pages)) continue;       // such a block is NaN in any case
-      const int64_t at = page_row_offset(a.pool, id, key, kvh) + (int64_t)E * lane * sizeof(CT);
-      float s = 0.f;
+    for (int k0 = first; k0 < end; k0 += U) {
+      float s[U], v[U][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) s = fmaf(q[e], elem(a.pool.k + at, e), s);
-      const float p = __builtin_amdgcn_exp2f(fmaf(wave_sum(s), sl2, -m));
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = row_at(min(k0 + u, end - 1));
+        s[u] = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(p, elem(a.pool.v + at, e), acc[e]);
+        for (int e = 0; e < E; ++e) {
+          s[u] = fmaf(q[e], elem(a.pool.k + at, e), s[u]);
+          v[u][e] = elem(a.pool.v + at, e);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(wave_sum(s[u]), sl2, -m));
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = k0 + u < end ? fmaf(p, v[u][e], acc[e]) : acc[e];
+      }
     }
     if (a.n_split == 1) {
       T* op = static_cast<T*>(a.out.p) + b * a.out.b + t * a.out.t + head * a.out.h + E * lane;
 #pragma unroll
-      for (int e = 0; e < E; ++e) ActIO<T>::store(op + e, acc[e] * (vs / l));
+      for (int e = 0; e < E; ++e) ActIO<T>::store(op + e, l == 0.f ? 0.f : acc[e] * (vs / l));
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) a.part[((grow + rr) * a.n_split + split) * D + E * lane + e] = acc[e];

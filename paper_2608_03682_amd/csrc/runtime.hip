@@ -1834,6 +1834,7 @@ int phyai_prefill_paged(phyai_expert* e, const float* embeds, const phyai_paged_
     if (causal != 0 && causal != 1) fail(PHYAI_EINVAL, "causal must be 0 or 1");
     if (!embeds || !past_len || !new_len) fail(PHYAI_EINVAL, "NULL argument");
     if ((reinterpret_cast<uintptr_t>(embeds) & 15u) != 0) fail(PHYAI_EINVAL, "embeds must be 16-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(status) & 3u) != 0) fail(PHYAI_EINVAL, "status must be 4-byte aligned");
     const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
     CallDesc hn{}, hp{}, hk{};
     int max_kv = 1;

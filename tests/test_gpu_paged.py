@@ -214,6 +214,47 @@ def test_what_a_row_does_not_see_does_not_reach_it(kind, rows):
     assert np.isfinite(clean).all()
 
 
+@pytest.mark.parametrize("rows", [3, 50])
+def test_a_value_that_rows_see_stays_what_it_is(rows):
+    """An infinite and a NaN value in a token that every row sees: those dimensions are
+    infinite and NaN, the others what they are without them (both shapes, split and not)."""
+    D, kv = 128, [700]
+    c = Cache(18, "bf16", 1, D, 16, kv)
+    q = (1.5 * torch.randn(1, rows, 4, D, generator=torch.Generator().manual_seed(5))).bfloat16().cuda()
+    page, at = c.host_table[0, 100 // 16], 100 % 16
+    for max_kv in (700, None):
+        c.v[page, at, 0, 5], c.v[page, at, 0, 9] = 0.0, 0.0
+        want = px().paged_attention(q, c.px, ints(kv), max_kv_len=max_kv)
+        c.v[page, at, 0, 5], c.v[page, at, 0, 9] = float("inf"), float("nan")
+        got = px().paged_attention(q, c.px, ints(kv), max_kv_len=max_kv)
+        rest = [d for d in range(D) if d not in (5, 9)]
+        assert torch.isposinf(got[..., 5]).all() and got[..., 9].isnan().all()
+        assert torch.equal(got[..., rest], want[..., rest])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_without_a_key_are_zero_beside_infinite_values(kind):
+    """More rows than keys: the first rows see none, and NaN in the keys that the others
+    see does not reach them."""
+    for rows, heads in ((6, 2), (60, 3)):
+        c = Cache(19, kind, 1, 64, 16, [5, 20])
+        for b, p in ((0, 4), (1, 19)):
+            page = c.host_table[b, p // 16]
+            y = c.v[page, p % 16].float()
+            y[:, 7] = float("nan")
+            c.v[page, p % 16] = y.to(c.v.dtype)
+        q = torch.ones(2, rows, heads, 64, device="cuda", dtype=torch.float32 if kind == "f32" else torch.bfloat16)
+        for max_kv in (20, None):
+            got = px().paged_attention(q, c.px, ints([5, 20]), max_kv_len=max_kv)
+            for b, n in enumerate((5, 20)):
+                if rows > n:
+                    assert (got[b, :rows - n] == 0).all()
+                last = got[b, rows - 1]
+                assert last[:, 7].isnan().all() and torch.isfinite(last[:, :7]).all() and torch.isfinite(last[:, 8:]).all()
+                if n > 1:                            # the row before the last does not see the NaN
+                    assert torch.isfinite(got[b, rows - 2]).all()
+
+
 def test_large_scores_and_zero_scales():
     """Scores of thousands (one key takes all), and an 8-bit cache whose keys have scale 0."""
     c = Cache(7, "f32", 1, 64, 16, [90])

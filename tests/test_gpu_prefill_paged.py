@@ -175,3 +175,26 @@ def test_arguments_are_checked():
     p, r = int(c.page_table[1, 0]), int(good.page_table[1, 0])
     assert torch.equal(c.k[:, p, :5], good.k[:, r, :5]) and torch.equal(c.v[:, p, :5], good.v[:, r, :5])
     lm.close()
+
+
+def test_gemma_size_in_two_chunks():
+    """The 18-layer model over 816 tokens: one block against phyai_prefill (two roundings
+    of the same values), and 768 image tokens, then 48 of text, with the image tokens'
+    keys and values those of a prefix of 768."""
+    cfg = wl.CONFIGS["plm_gemma_bf16_b1"]
+    case = wl.make_prefill_case(cfg, seed=0)
+    lm = px().PrefixLM(cfg, case.weights)
+    emb = torch.from_numpy(case.embeds).cuda()
+    want = lm.prefill(emb, [816]).view(torch.bfloat16).double()
+    one = chunked(cfg, case, 1, [816], [[816]], [False], 64, lm=lm).double()
+    two = chunked(cfg, case, 1, [816], [[768, 48]], [False, True], 64, lm=lm).double()
+    short = lm.prefill(emb, [768]).view(torch.bfloat16).double()[:, :, :, :768]
+    lm.close()
+    for l in range(cfg.n_layers):
+        w = want[l].cpu().numpy()
+        bar = 2 * kv_bar(cfg.replace(n_layers=l + 1), w)
+        print(f"[parity] layer {l}: one block {np.abs(one[l].cpu().numpy() - w).max():.3e}, bar {bar:.3e}", flush=True)
+        assert np.abs(one[l].cpu().numpy() - w).max() <= bar
+        s = short[l].cpu().numpy()
+        assert np.abs(two[l, :, :, :768].cpu().numpy() - s).max() <= 2 * kv_bar(cfg.replace(n_layers=l + 1), s)
+    assert torch.isfinite(two).all()

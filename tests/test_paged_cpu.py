@@ -113,6 +113,19 @@ def test_norm_rope_refuses():
         refused(nr(**kw), needle)
 
 
+def test_misaligned_words_are_refused():
+    """Lengths, scales and the status word (an atomic on a misaligned word faults)."""
+    L, r, odd = px.lib(), ctypes.byref, P + 2
+    refused(attend(kv=odd), "4-byte")
+    refused(attend(new=odd), "4-byte")
+    refused(attend(cache(dtype=2, k_scale=odd, v_scale=P)), "4-byte")
+    refused(L.phyai_paged_attention(r(cache()), 0, r(rows(8)), r(rows(8)), P, None, 256, 0.1, 1, 0, 4, 1, P, 1 << 40, odd, None), "4-byte")
+    refused(L.phyai_paged_append(r(cache()), 0, r(rows(2)), r(rows(2)), 0.0, odd, None, 4, 1, None, None), "4-byte")
+    refused(L.phyai_paged_append(r(cache()), 0, r(rows(2)), r(rows(2)), 0.0, P, None, 4, 1, odd, None), "4-byte")
+    refused(L.phyai_paged_gather(r(cache()), P, P, 16, odd, None), "4-byte")
+    refused(L.phyai_qk_norm_rope(r(rows(8)), None, r(rows(8)), None, None, None, 1e-6, 1e4, None, None, 2, 4, 128, 1, odd, None), "4-byte")
+
+
 def test_workspace_depends_on_the_split_alone():
     L, r = px.lib(), ctypes.byref
     # a chip full of rows: no split; one row over many keys: split
