@@ -33,6 +33,7 @@ namespace {
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int s32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // LDS by byte address
@@ -85,12 +86,15 @@ __device__ __forceinline__ float pair_sum(float x) {
 //   V   bf16: 32 lanes, which the LDS serves at once, read 64 bytes of each of 4
 //       rows, so rows 0 .. 3 differ in the bits above those 64 bytes; f32: 32 lanes
 //       read 128 bytes of one row, the other half of the row 4 further on
+//       8-bit codes: 32 lanes read 32 bytes of each of 8 rows (0 .. 3 and 8 .. 11)
 template <int RB>
-__device__ __forceinline__ int k_swz(int r) { return RB >= 256 ? (r & 15) : ((r >> 1) & 7); }
-template <int ES, int RB>
+__device__ __forceinline__ int k_swz(int r) { return RB >= 256 ? (r & 15) : RB >= 128 ? ((r >> 1) & 7) : ((r >> 2) & 3); }
+template <int VS, int RB>
 __device__ __forceinline__ int v_swz(int r) {
-  if (ES == 4) return 8 * ((r >> 2) & 1);
-  return RB >= 256 ? 4 * (r & 3) + 2 * ((r >> 2) & 1) : 4 * ((r >> 1) & 1) + 2 * ((r >> 2) & 1);
+  if (VS == 4) return 8 * ((r >> 2) & 1);
+  if (VS == 2) return RB >= 256 ? 4 * (r & 3) + 2 * ((r >> 2) & 1) : 4 * ((r >> 1) & 1) + 2 * ((r >> 2) & 1);
+  const int far = (r >> 3) & 1;
+  return RB >= 256 ? 2 * (r & 3) + 8 * far : RB >= 128 ? 2 * ((r >> 1) & 1) + 4 * far : 2 * far;
 }
 
 // Order of one MFMA loop whose operands come from LDS: PD reads ahead, then each
@@ -128,8 +132,14 @@ template <typename CT, typename T, int D, bool KEYS>
 struct Shape {
   static constexpr int ES = sizeof(T);
   static constexpr bool kFp8 = sizeof(CT) == 1;
-  static constexpr int RB = D * ES;                     // bytes of an LDS row
-  static constexpr int CPR = RB / 16;                   // chunks of a row
+  // An 8-bit pool's codes go into LDS as they are where one wave works on a tile, and
+  // are widened when the fragments are read; four waves would each widen all of them, so
+  // there the tile is widened once, on its way through registers.
+  static constexpr bool kCodes = kFp8 && KEYS, kRegs = kFp8 && !KEYS;
+  static constexpr int VS = kCodes ? 1 : ES;            // bytes of a value in LDS
+  static constexpr int RB = D * VS;                     // bytes of an LDS row
+  static constexpr int OB = D * ES;                     // bytes of a row of q and out
+  static constexpr int CPR = OB / 16;                   // chunks of it
   static constexpr int KT = (ES == 2 && !KEYS) ? 64 : 32;   // keys of a tile
   static constexpr int TILE = KT * RB;                  // bytes of a K or V tile
   static constexpr int NW = KEYS ? 1 : 4;
@@ -139,7 +149,7 @@ struct Shape {
   // rows: the scores run a tile ahead
   static constexpr bool kAhead = !KEYS && ES == 2 && D == 256;
   // waves of a SIMD asked for, and with them blocks of a CU
-  static constexpr int PER_SIMD = KEYS ? (RB <= 128 ? 4 : RB <= 256 ? 2 : 1) : (LDS <= 64 * 1024 ? 2 : 1);
+  static constexpr int PER_SIMD = KEYS ? (OB <= 128 ? 4 : OB <= 256 ? (kCodes ? 3 : 2) : 1) : (LDS <= 64 * 1024 ? 2 : 1);
   static constexpr int LDS_BLOCKS = 160 * 1024 / LDS;
   static constexpr int PER_CU = LDS_BLOCKS < 4 * PER_SIMD / NW ? LDS_BLOCKS : 4 * PER_SIMD / NW;
 };
@@ -148,9 +158,9 @@ template <typename CT, typename T, int D, bool KEYS, int NT = 64 * Shape<CT, T, 
           int PER_SIMD = Shape<CT, T, D, KEYS>::PER_SIMD>
 __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs a) {
   using S = Shape<CT, T, D, KEYS>;
-  constexpr int ES = S::ES, RB = S::RB, CPR = S::CPR, KT = S::KT, KB = KT / 32, TILE = S::TILE, NW = S::NW;
+  constexpr int ES = S::ES, VS = S::VS, RB = S::RB, OB = S::OB, CPR = S::CPR, KT = S::KT, KB = KT / 32, TILE = S::TILE, NW = S::NW;
   constexpr int V_AT = S::BUFS * TILE;                  // LDS: [K, V][buffer][TILE]
-  constexpr int ROWS = S::ROWS, NQ = RB / 32;           // chunk pairs of a row
+  constexpr int ROWS = S::ROWS, NQ = OB / 32;           // chunk pairs of a row
   // aligned so that the two buffers of a tile differ in one address bit
   __shared__ __attribute__((aligned(2 * TILE))) char sm[S::LDS];
   __shared__ int s_bad;
@@ -214,14 +224,16 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     return;
   }
 
-  // Q^T operand: chunk 2 s + h of the row
+  // Q^T operand: chunk 2 s + h of the row; with codes in LDS, where a lane reads 16 of a
+  // key at once, chunk 4 (s / 2) + 2 h + s % 2
   uint4 qf[NQ];
   {
-    const char* qp = static_cast<const char*>(a.q.p) + (b * a.q.b + tok * a.q.t + qhead * a.q.h) * ES + 16 * hl;
+    const char* qp = static_cast<const char*>(a.q.p) + (b * a.q.b + tok * a.q.t + qhead * a.q.h) * ES +
+                     (S::kCodes ? 32 : 16) * hl;
 #pragma unroll
     for (int s = 0; s < NQ; ++s) {
       qf[s] = make_uint4(0, 0, 0, 0);
-      if (valid) qf[s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
+      if (valid) qf[s] = *reinterpret_cast<const uint4*>(qp + (S::kCodes ? 64 * (s / 2) + 16 * (s % 2) : 32 * s));
     }
   }
 
@@ -257,7 +269,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     return page * static_cast<uint64_t>(a.pool.page_bytes);
   };
 
-  constexpr int GB = S::kFp8 ? D : RB;                  // bytes of a row in its page
+  constexpr int GB = S::kFp8 ? D : OB;                  // bytes of a row in its page
   constexpr int LPR = GB / 16;                          // lanes of a row
   constexpr int RPI = kWave / LPR;                      // rows of one load instruction
   constexpr int NLD = KT / RPI / NW;                    // load instructions of a wave, per operand
@@ -269,9 +281,9 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const int lrow = lane / LPR, wrow0 = wave * RPI;
   auto row_of = [&](int i) { return NW * i * RPI; };   // first_row(i) - wrow0
   const uint32_t lane_row = static_cast<uint32_t>(lrow) * a.pool.token_bytes;
-  const uint32_t kc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : k_swz<RB>(wrow0 + lrow)));
-  const uint32_t vc = 16 * ((lane % LPR) ^ (S::kFp8 ? 0 : v_swz<ES, RB>(wrow0 + lrow)));
-  uint4 kr[S::kFp8 ? NLD : 1], vr[S::kFp8 ? NLD : 1];
+  const uint32_t kc = 16 * ((lane % LPR) ^ (S::kRegs ? 0 : k_swz<RB>(wrow0 + lrow)));
+  const uint32_t vc = 16 * ((lane % LPR) ^ (S::kRegs ? 0 : v_swz<VS, RB>(wrow0 + lrow)));
+  uint4 kr[S::kRegs ? NLD : 1], vr[S::kRegs ? NLD : 1];
   // The window holds the pages of keys from .. to (fewer than 64 pages), `from` and later
   // ones being all that is still needed.
   auto cover = [&](int from, int to) {
@@ -280,9 +292,9 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const int big_page = a.pool.page_shift >= (KT == 64 ? 6 : 5);   // a page holds whole tiles
   const uint32_t token_bytes = a.pool.token_bytes;
   auto load = [&](bool is_v, uint32_t buf, int i, const char* p, uint32_t row_off) {
-    const uint32_t off = row_off + (is_v ? vc ^ (S::kFp8 ? 0 : 16 * v_swz<ES, RB>(row_of(i)))
-                                         : kc ^ (S::kFp8 ? 0 : 16 * k_swz<RB>(row_of(i))));
-    if constexpr (S::kFp8) (is_v ? vr : kr)[i] = *reinterpret_cast<const uint4*>(p + off);
+    const uint32_t off = row_off + (is_v ? vc ^ (S::kRegs ? 0 : 16 * v_swz<VS, RB>(row_of(i)))
+                                         : kc ^ (S::kRegs ? 0 : 16 * k_swz<RB>(row_of(i))));
+    if constexpr (S::kRegs) (is_v ? vr : kr)[i] = *reinterpret_cast<const uint4*>(p + off);
     else dma16(p, off, lds0 + buf + (is_v ? V_AT : 0) + (wrow0 + row_of(i)) * RB);
   };
   auto issue = [&](bool is_v, uint32_t buf, int k0) {
@@ -309,11 +321,11 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   };
   // what was issued last for K or V is complete and in LDS
   auto commit = [&](bool is_v, uint32_t buf) {
-    if constexpr (S::kFp8) {
+    if constexpr (S::kRegs) {
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
         const int r = wrow0 + row_of(i) + lrow, c = 2 * (lane % LPR);
-        const int sw = is_v ? v_swz<ES, RB>(r) : k_swz<RB>(r);
+        const int sw = is_v ? v_swz<VS, RB>(r) : k_swz<RB>(r);
         const uint4 w = (is_v ? vr : kr)[i];
         char* row = sm + buf + (is_v ? V_AT : 0) + r * RB;
         *reinterpret_cast<bf16x8*>(row + 16 * (c ^ sw)) = fp8x8_to_bf16x8(w.x, w.y);
@@ -335,19 +347,28 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   // Fragment addresses: chunk 2 s + h of K row lr is at k_at ^ 32 s, the V^T operand
   // of dims 32 db + lr in the key order of the accumulators at v_at ^ (64 db) (bf16,
   // four keys a read) or v_at ^ (128 db) (f32, one key), plus whole rows.
-  const int i16 = lane % 16, vr0 = ES == 2 ? 4 * hl + i16 / 4 : 4 * hl;
+  // codes: eight keys a read, at v_at ^ (32 db)
+  const int i16 = lane % 16, half16 = (lane / 16) % 2;
+  const int vr0 = S::kCodes ? 8 * (i16 / 8) + 4 * hl + i16 / 2 % 4 : ES == 2 ? 4 * hl + i16 / 4 : 4 * hl;
   const uint32_t k_at = lds0 + lr * RB + 16 * (hl ^ k_swz<RB>(lr));
   const uint32_t v_at =
       lds0 + V_AT + vr0 * RB +
-      (ES == 2 ? 16 * ((2 * ((lane / 16) % 2) + (i16 % 4) / 2) ^ v_swz<ES, RB>(vr0)) + 8 * (i16 & 1)
-               : 16 * ((lr / 4) ^ v_swz<ES, RB>(vr0)) + 4 * (lr % 4));
+      (S::kCodes ? 16 * (half16 ^ v_swz<VS, RB>(vr0)) + 8 * (i16 & 1)
+       : ES == 2 ? 16 * ((2 * half16 + (i16 % 4) / 2) ^ v_swz<VS, RB>(vr0)) + 8 * (i16 & 1)
+                 : 16 * ((lr / 4) ^ v_swz<VS, RB>(vr0)) + 4 * (lr % 4));
   auto v_bf16 = [&](uint32_t at, int t, int db) {
-    union { s16x4 h[2]; bf16x8 v; } f;
+    if constexpr (S::kCodes) {
+      const s32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+          reinterpret_cast<__attribute__((address_space(3))) s32x2*>((at ^ (32u * db)) + 16 * t * RB));
+      return fp8x8_to_bf16x8(w.x, w.y);
+    } else {
+      union { s16x4 h[2]; bf16x8 v; } f;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      f.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          reinterpret_cast<__attribute__((address_space(3))) s16x4*>((at ^ (64u * db)) + (16 * t + 8 * j) * RB));
-    return f.v;
+      for (int j = 0; j < 2; ++j)
+        f.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            reinterpret_cast<__attribute__((address_space(3))) s16x4*>((at ^ (64u * db)) + (16 * t + 8 * j) * RB));
+      return f.v;
+    }
   };
   auto v_f32 = [&](uint32_t at, int kb, int v, int db) {
     return lds_at<float>((at ^ (128u * db)) + (32 * kb + 8 * (v / 4) + v % 4) * RB);
@@ -361,12 +382,15 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
 #pragma unroll
       for (int v = 0; v < 16; ++v) st[kb][v] = 0.f;
 #pragma unroll
-    for (int s = 0; s < NQ; ++s)
+    for (int s = 0; s < NQ; s += S::kCodes ? 2 : 1)
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        const u32x4 kv4 = lds_at<u32x4>((ka ^ (32u * s)) + 32 * kb * RB);
+        const u32x4 kv4 = lds_at<u32x4>((ka ^ (S::kCodes ? 16u * s : 32u * s)) + 32 * kb * RB);
         const uint4 kf = make_uint4(kv4.x, kv4.y, kv4.z, kv4.w);
-        if constexpr (ES == 2) {
+        if constexpr (S::kCodes) {
+          st[kb] = mfma32x32x16(fp8x8_to_bf16x8(kf.x, kf.y), as_bf16x8(qf[s]), st[kb]);
+          st[kb] = mfma32x32x16(fp8x8_to_bf16x8(kf.z, kf.w), as_bf16x8(qf[s + 1]), st[kb]);
+        } else if constexpr (ES == 2) {
           st[kb] = mfma32x32x16(as_bf16x8(kf), as_bf16x8(qf[s]), st[kb]);
         } else {
           st[kb] = mfma_f32(__uint_as_float(kf.x), __uint_as_float(qf[s].x), st[kb]);
@@ -517,7 +541,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     if (kbeg < kend) {
       auto wait = [&](bool last) {                      // all loads but the youngest tile's
         if (last) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(S::kFp8 ? 63 : NLD) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NLD) : "memory");
       };
       // other lanes read what a lane wrote, and loads overwrite what lanes have read: LDS
       // operations of a wave complete in order, the compiler has to keep that order
@@ -525,14 +549,13 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       load_pages(kbeg >> a.pool.page_shift);
       issue(false, 0, kbeg);
       issue(true, 0, kbeg);
-      if constexpr (S::kFp8) commit(false, 0);
       wait(false);
       for (int k0 = kbeg;; k0 += KT) {
         const bool more = k0 + KT < kend;
         f32x16 st[KB];
         bf16x8 pf[2 * KB];
         scores(st, 0);
-        if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
+        if constexpr (VS == 2) mfma_pipeline<KB * NQ, 1, 4>();
         fence();
         if (more) {
           cover(k0 + KT, k0 + 2 * KT);
@@ -542,14 +565,12 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
         hide(st, half, k0);
         rescale(half);
         weights(st, pf);
-        if constexpr (S::kFp8) commit(true, 0);
         wait(!more);
         values(st, pf, 0);
-        if constexpr (ES == 2) mfma_pipeline<2 * KB * (D / 32), 2, 2>();
+        if constexpr (VS == 2) mfma_pipeline<2 * KB * (D / 32), 2, 2>();
         if (!more) break;
         fence();
         issue(true, 0, k0 + KT);
-        if constexpr (S::kFp8) commit(false, 0);
         wait(false);
       }
     }
@@ -730,8 +751,8 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   } else {
     // whole rows through LDS, so that a store instruction covers 1 KiB of them
     const float inv = l_run == 0.f ? 0.f : vs / l_run;
-    char* stage = sm + wave * 32 * RB;
-    static_assert(S::LDS >= NW * 32 * RB, "the output is staged in the tiles");
+    char* stage = sm + wave * 32 * OB;
+    static_assert(S::LDS >= NW * 32 * OB, "the output is staged in the tiles");
     constexpr int SW = CPR < 16 ? CPR - 1 : 15;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
@@ -739,7 +760,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       for (int u = 0; u < 4; ++u) {
         const float v4[4] = {o[db][4 * u] * inv, o[db][4 * u + 1] * inv, o[db][4 * u + 2] * inv, o[db][4 * u + 3] * inv};
         const int byte = (32 * db + 8 * u + 4 * hl) * ES;
-        ActIO<T>::store4(reinterpret_cast<T*>(stage + lr * RB + 16 * ((byte / 16) ^ (lr & SW)) + byte % 16), v4);
+        ActIO<T>::store4(reinterpret_cast<T*>(stage + lr * OB + 16 * ((byte / 16) ^ (lr & SW)) + byte % 16), v4);
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     constexpr int RPS = kWave / CPR > 0 ? kWave / CPR : 1;
@@ -748,7 +769,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       const int r = RPS * i + lane / CPR, c = lane % CPR;
       const int rr = wrow + r;
       if (rr < rows) {
-        const uint4 w = *reinterpret_cast<const uint4*>(stage + r * RB + 16 * (c ^ (r & SW)));
+        const uint4 w = *reinterpret_cast<const uint4*>(stage + r * OB + 16 * (c ^ (r & SW)));
         char* op = reinterpret_cast<char*>(static_cast<T*>(a.out.p) + b * a.out.b + (rr / G) * a.out.t +
                                            (kvh * G + rr % G) * a.out.h);
         *reinterpret_cast<uint4*>(op + 16 * c) = w;
