@@ -14,11 +14,20 @@
 // one column.
 //
 // Two shapes of block:
-//   rows   NW waves x 32 query rows, K/V tiles shared by the waves: chunks, which
-//          are bound by the matrix cores and the exponentials;
+//   rows   four waves x 32 query rows that share K/V tiles, the next tile under way in a
+//          second buffer: chunks.  Bound by the matrix cores and what goes on beside them:
+//          4,096 rows of 32 heads over 8,192 keys of 128, causal, take 418 .. 449 us from box
+//          to box (920 .. 987 TFLOP/s; the library's product of 8,192^3 reaches 1,116 there),
+//          the matrix cores busy 49 % of the cycles, the LDS 25 %, with 0.5 % of those in
+//          conflict.  At head_dim 256 a CU has one wave a SIMD, and the scores run a tile
+//          ahead so that products and exponentials overlap inside the wave.
 //   keys   one wave on 32 rows, one tile of K and of V in LDS, many waves a CU: few
-//          rows, which are bound by reading K/V.
-// Either may split the keys over blocks; a second kernel joins the splits.
+//          rows, which are bound by reading K/V: 64 requests of one token over 600 .. 4,000
+//          keys 124 us (4.9 TB/s; a large copy moves 4.8, a read alone 6.5), 131,072 keys in
+//          8 bits 167 us (5.6 TB/s), one request over 817 keys 12 us, of which the two
+//          launches are about seven.
+// Either may split the keys over blocks; a second kernel joins the splits (25 us for 64
+// splits of 128 rows with one wave a row, 6.5 with four).
 #include "common.hpp"
 #include "errors.hpp"
 #include "paged.hpp"
@@ -848,9 +857,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, bool f
   for (int e = 0; e < E; ++e) ActIO<T>::store(op + e, acc[e] * inv);
 }
 
-// Few rows: every wave reads keys of its own.  More than 64 rows of a K/V head would
-// read the keys three times and more.
-bool keys_shape(const PagedAttnArgs& a) { return a.M * a.G <= 64; }
+// Which shape: of few rows the keys shape, whose waves each stream keys of their own, of
+// more the rows shape, whose four waves share a tile.  Figures in us, keys | rows shape:
+//   bf16, head_dim 128, 32 requests over 4,096 keys, 8 K/V heads: 4 rows 114 | 110, 8 rows
+//     120 | 115, 16 rows 129 | 118, 32 rows 146 | 121; 64 ragged requests of 4 rows 128 | 144, of 8
+//     rows of 256: 41 | 56; eight requests: 4 rows 30.9 | 31.3, 16 rows 35.8 | 32.6; one request:
+//     4 rows 12.1 | 12.4, 32 rows 14.4 | 15.3.
+//   8 bits, the same: 4 rows 64 | 78, 8 rows 69 | 79, 16 rows 78 | 80, 32 rows 93 | 83.
+//   32 bits, bound by its products, of which the rows shape does those of 128 rows
+//     whatever there are: 64 requests of 4 rows 179 | 520, 4 requests over 2,048 keys of 32
+//     rows 25 | 30, of 64 rows 29 | 33, of 128 rows 39 | 39.  At head_dim 256 a wave's rows,
+//     accumulators and a tile exceed its registers: 4 rows 61 | 48, 64 requests 1,134 | 1,085;
+//     there is no keys shape for it.
+template <typename CT, typename T, int D>
+constexpr int kKeysRows = sizeof(T) == 4 ? (D == 256 ? 0 : 64) : sizeof(CT) == 1 ? 16 : 8;
 
 template <typename CT, typename T, int D, bool KEYS>
 void launch(const PagedAttnArgs& a, hipStream_t s) {
@@ -866,8 +886,9 @@ void launch(const PagedAttnArgs& a, hipStream_t s) {
 
 template <typename CT, typename T, int D>
 void launch_shape(const PagedAttnArgs& a, hipStream_t s) {
-  if (keys_shape(a)) launch<CT, T, D, true>(a, s);
-  else launch<CT, T, D, false>(a, s);
+  if constexpr (kKeysRows<CT, T, D> > 0)
+    if (a.M * a.G <= kKeysRows<CT, T, D>) return launch<CT, T, D, true>(a, s);
+  launch<CT, T, D, false>(a, s);
 }
 
 template <typename CT, typename T, int D, bool KEYS>
@@ -915,8 +936,9 @@ void plan(PagedAttnArgs& a) {
 
 template <typename CT, typename T, int D>
 void plan_shape(PagedAttnArgs& a) {
-  if (keys_shape(a)) plan<CT, T, D, true>(a);
-  else plan<CT, T, D, false>(a);
+  if constexpr (kKeysRows<CT, T, D> > 0)
+    if (a.M * a.G <= kKeysRows<CT, T, D>) return plan<CT, T, D, true>(a);
+  plan<CT, T, D, false>(a);
 }
 
 template <typename F>
