@@ -424,10 +424,10 @@ typedef struct {
  *   rope_base     >= 1: rotate; 0: normalise only.
  *   past_len      device [batch], or NULL (0).   new_len  device [batch], or NULL (rows).
  *   dtype         F32 or BF16 of every row.  Sums, norms and angles are held in 32
- *                 bits or more (angles exact to 2^-31 of a turn at any position).
+ *                 bits or more (angles good to 2^-25 of a turn at any position).
  *
- * A request whose lengths are out of range (new_len outside 0..rows, past_len < 0) is
- * not touched (PHYAI_PAGED_BAD_LENGTH). */
+ * batch * rows is at most 2^24.  A request whose lengths are out of range (new_len
+ * outside 0..rows, past_len < 0) is not touched (PHYAI_PAGED_BAD_LENGTH). */
 int phyai_qk_norm_rope(const phyai_head_rows* q, const phyai_head_rows* k, const phyai_head_rows* q_out,
                        const phyai_head_rows* k_out, const float* q_gain, const float* k_gain, float eps,
                        float rope_base, const int32_t* past_len, const int32_t* new_len, int32_t batch,
@@ -437,7 +437,8 @@ int phyai_qk_norm_rope(const phyai_head_rows* q, const phyai_head_rows* k, const
  * request b goes to token past_len[b] + t, the key rotated to that position on the
  * way (rope_base >= 1; 0: stored as it is).  The cache of dtype F32 takes F32
  * rows, BF16 and FP8E4M3 take BF16 rows; 8-bit codes are value / scale to the
- * nearest, ties to even, saturated at 448.
+ * nearest, ties to even, saturated at 448 (0 over a scale of 0 is 0).  batch * rows is
+ * at most 2^24.
  *
  * Not written: requests with past_len + new_len beyond max_pages * page_size or a
  * length out of range (PHYAI_PAGED_BAD_LENGTH), tokens whose page number is out of
@@ -492,8 +493,8 @@ int phyai_paged_gather(const phyai_paged_cache* cache, const int32_t* kv_len, vo
 
 /* phyai_prefill chunk by chunk over a paged cache (handle of variant
  * PHYAI_VARIANT_PREFIX_LM): the keys and values of each request's next tokens, of every
- * layer, are appended to its pages after the tokens have attended, layer by layer, to
- * what the request has in the cache and to one another.  One chunk of a whole
+ * layer, are appended to its pages, and the tokens attend, layer by layer, to what the
+ * request has in the cache and to one another.  One chunk of a whole
  * prefix with causal = 0 leaves, after phyai_paged_gather, what phyai_prefill computes;
  * later chunks (text that arrives after the images, single tokens) see the earlier
  * ones and are not seen by them.

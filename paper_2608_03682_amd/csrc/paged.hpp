@@ -18,7 +18,7 @@ enum PagedStatus { PAGED_BAD_PAGE = 1, PAGED_BAD_LENGTH = 2 };
 
 // The angle of pair i at position p is p * base^(-2i/D).  freq[i] holds
 // base^(-2i/D) / 2 pi turns as a 64-bit fraction of a turn, so p * freq[i] mod 2^64
-// is the angle with the whole turns taken off, exact to p * 2^-65 of a turn: a
+// is the angle with the whole turns taken off, good to p * (2^-64 + 2^-55 of freq): a
 // float32 product would be off by 0.06 rad at a position of 10^6.
 constexpr int kMaxPairs = 128;
 struct RopeFreq {

@@ -41,6 +41,11 @@ void check_sizes(int batch, int rows, int dim) {
   req((int64_t)batch * rows <= INT32_MAX / 2, "batch * rows out of range");
 }
 
+// A block of 256 threads takes one or two tokens, and a launch has fewer than 2^32 threads.
+void check_tokens(int batch, int rows) {
+  req((int64_t)batch * rows <= (1 << 24), "batch * rows out of range 1..2^24");
+}
+
 HeadRows head_rows(const phyai_head_rows* h, int dtype, const char* what) {
   const int es = elem_bytes(dtype);
   const std::string w = what;
@@ -62,7 +67,7 @@ HeadRows out_rows(const phyai_head_rows* h, int dtype, const char* what, int bat
 }
 
 // base^(-2i/D) turns over 2 pi as 64-bit fractions.  The powers are multiplied up in
-// long double (64-bit mantissa): 128 factors lose 2^-57 at most.
+// long double (64-bit mantissa): 128 factors lose 2^-55 of the value at most.
 bool rope_freq(float base, int D, RopeFreq& f) {
   for (auto& x : f.f) x = 0;
   req(base == 0.f || (std::isfinite(base) && base >= 1.f), "rope_base must be 0 or a number >= 1");
@@ -127,6 +132,7 @@ void enqueue_norm_rope(const phyai_head_rows* q, const phyai_head_rows* k, const
                        int head_dim, int dtype, int32_t* status, hipStream_t s) {
   const int kind = row_kind(dtype);
   check_sizes(batch, rows, head_dim);
+  check_tokens(batch, rows);
   req(q || k, "q and k are both NULL");
   NormRopeArgs a{};
   if (q) {
@@ -167,6 +173,7 @@ void enqueue_append(const phyai_paged_cache* cache, int layer, const phyai_head_
   const int kind = row_kind(dtype);
   req((kind == PAGED_F32) == (cache->dtype == PHYAI_DTYPE_F32), "an F32 cache takes F32 rows, BF16 and FP8E4M3 caches BF16 rows");
   check_sizes(cache->batch, rows, cache->head_dim);
+  check_tokens(cache->batch, rows);
   a.k = head_rows(k, dtype, "k");
   a.v = head_rows(v, dtype, "v");
   req(a.k.n == cache->n_kv_heads && a.v.n == cache->n_kv_heads, "k and v must have the cache's n_kv_heads heads");

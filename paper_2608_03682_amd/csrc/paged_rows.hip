@@ -48,12 +48,13 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// e4m3 codes, to the nearest, ties to even; what lies beyond 448 becomes 448, NaN stays
+// e4m3 codes, to the nearest, ties to even; what lies beyond 448 becomes 448, NaN stays.
+// 0 is 0 over a scale of 0 too, which a head of zeros has by its largest magnitude.
 __device__ __forceinline__ float sat_fp8(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
 __device__ __forceinline__ void store8_fp8(uint8_t* p, const float (&v)[8], float scale) {
   float q[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = sat_fp8(v[i] / scale);
+  for (int i = 0; i < 8; ++i) q[i] = sat_fp8(v[i] == 0.f ? v[i] : v[i] / scale);
   uint32_t w[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -64,7 +65,8 @@ __device__ __forceinline__ void store8_fp8(uint8_t* p, const float (&v)[8], floa
 }
 
 // cos and sin of position * freq turns.  The product modulo one turn is exact in
-// 64 bits; its upper 32, as a signed fraction of a turn, is what the sine takes.
+// 64 bits; its upper 32, as a signed fraction of a turn rounded to float32 (2^-26 of a
+// turn at most), is what the sine takes.
 __device__ __forceinline__ float2 turn(uint64_t freq, int pos) {
   const uint64_t p = freq * static_cast<uint64_t>(pos);
   const float half_turns = static_cast<float>(static_cast<int32_t>(p >> 32)) * 0x1p-31f;

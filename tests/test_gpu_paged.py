@@ -10,7 +10,7 @@ h = 2^-8, that of bfloat16, each relative to the value):
                bf16, fp8  the same, plus h m for the weights' rounding and h |o| for
                           the output's
   norm       the sum of squares is off by (D + 4) u, its root by half of that; gain,
-             rotation and angle (2^-31 of a turn) add 16 u: ((D + 4) / 2 + 16) u (|a| + |b|)
+             rotation and angle (2^-25 of a turn, 3.2 u) add 16 u: ((D + 4) / 2 + 16) u (|a| + |b|)
              over the pair, plus h |y| for bf16
   append     values are stored exactly; rotated keys 16 u (|a| + |b|), plus h |y| for bf16;
              8 bits: half a step of the code (2^-4 of the value, 2^-10 below the
@@ -468,6 +468,26 @@ def test_append_and_gather_skip_what_is_out_of_range():
     assert status.item() == px().PAGED_BAD_PAGE | px().PAGED_BAD_LENGTH
     assert g[0, :, 0, 16:].isnan().all() and g[0, 0, 0, :16].equal(c.k[t[0, 0], :, 0])
     assert g[0, :, 1].isnan().all() and g[0, :, 3].isnan().all() and (g[0, :, 2, 20:] == 0).all()
+
+
+def test_a_scale_of_zero_holds_zeros():
+    """A head of zeros whose scale is its largest magnitude / 448: codes of 0, not of 0 / 0; NaN stays NaN."""
+    D, nkv, ps = 128, 2, 16
+    pools = torch.full((2, 2, ps, nkv, D), 0x55, dtype=torch.uint8, device="cuda")
+    k_scale, v_scale = torch.tensor([0.0, 0.5], device="cuda"), torch.tensor([0.5, 0.0], device="cuda")
+    c = px().PagedCache(pools[0], pools[1], ints([[1]]), k_scale, v_scale)
+    k, v = torch.zeros(2, 1, 3, nkv, D, dtype=torch.bfloat16, device="cuda")
+    k[0, 2, 0, 5] = float("nan")
+    for base in (0.0, 1e4):
+        px().paged_append(c, k, v, ints([0]), rope_base=base)
+        got = pools[:, 1, :3].cpu()
+        for pool in (0, 1):
+            assert ((got[pool, :2] & 0x7f) == 0).all()
+        assert (got[0, 2, 0, 5] & 0x7f) == 0x7f and ((got[1, 2] & 0x7f) == 0).all()
+    out = px().paged_gather(c, ints([2]), 2)
+    assert (out == 0).all()
+    q = torch.ones(1, 1, 4, D, dtype=torch.bfloat16, device="cuda")
+    assert (px().paged_attention(q, c, ints([2])) == 0).all()
 
 
 def test_a_shared_page_and_the_same_request_twice():

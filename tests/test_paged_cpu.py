@@ -113,6 +113,15 @@ def test_norm_rope_refuses():
         refused(nr(**kw), needle)
 
 
+def test_more_tokens_than_a_launch_holds_are_refused():
+    """One block of 256 threads for every two tokens at least, and a launch has fewer than 2^32 threads."""
+    L, r, wide = px.lib(), ctypes.byref, (1 << 24) // 32 + 1
+    many = rows(2, b=1 << 30)
+    refused(L.phyai_qk_norm_rope(r(many), None, r(many), None, None, None, 0.0, 1e4, P, None, 32, wide, 128, 1, None, None),
+            "batch * rows")
+    refused(L.phyai_paged_append(r(cache(batch=32)), 0, r(many), r(many), 0.0, P, None, wide, 1, None, None), "batch * rows")
+
+
 def test_misaligned_words_are_refused():
     """Lengths, scales and the status word (an atomic on a misaligned word faults)."""
     L, r, odd = px.lib(), ctypes.byref, P + 2
