@@ -122,6 +122,7 @@ struct PagedAttnArgs {
   float* part;              // n_split > 1: [B][nkv][M * G][n_split][D], not normalised
   float2* ml;               // and each split's (maximum, sum): [B][nkv][M * G][n_split]
   int B, M, nkv, G, max_kv, causal, window, n_split, split_keys, n_tiles;
+  int pairs;                // 1: chunks in blocks of which a CU holds two
   float scale;
 };
 

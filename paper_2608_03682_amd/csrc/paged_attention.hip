@@ -13,7 +13,7 @@
 // token-major in their pages; the transposing LDS read hands each lane four keys of
 // one column.
 //
-// Two shapes of block:
+// Three shapes of block:
 //   rows   four waves x 32 query rows that share K/V tiles, the next tile under way in a
 //          second buffer: chunks.  Bound by the matrix cores and what goes on beside them:
 //          4,096 rows of 32 heads over 8,192 keys of 128, causal, take 418 .. 449 us from card
@@ -21,6 +21,9 @@
 //          the matrix cores busy 49 % of the cycles, the LDS 25 %, with 0.5 % of those in
 //          conflict.  At head_dim 256 a CU has one wave a SIMD, and the scores run a tile
 //          ahead so that products and exponentials overlap inside the wave.
+//   pairs  the same of bf16 at head_dim 256 with tiles of 32 keys: registers and LDS of two
+//          blocks a CU, whose waves overlap each other instead.  2,048 rows of 8 heads over
+//          8,192 keys: 155 us, the rows shape 170.
 //   keys   one wave on 32 rows, one tile of K and of V in LDS, many waves a CU: few
 //          rows, which are bound by reading K/V: 64 requests of one token over 600 .. 4,000
 //          keys 124 us (4.9 TB/s; a large copy moves 4.8, a read alone 6.5), 131,072 keys in
@@ -137,8 +140,11 @@ __device__ __forceinline__ void mfma_settle() {
 
 // What a block of one kind looks like.  CT: element of the pool, T: of the rows
 // and of the products.
-template <typename CT, typename T, int D, bool KEYS>
+enum Block { kRows, kKeys, kPairs };
+
+template <typename CT, typename T, int D, Block BLK>
 struct Shape {
+  static constexpr bool KEYS = BLK == kKeys;
   static constexpr int ES = sizeof(T);
   static constexpr bool kFp8 = sizeof(CT) == 1;
   // An 8-bit pool's codes go into LDS as they are where one wave works on a tile, and
@@ -149,24 +155,25 @@ struct Shape {
   static constexpr int RB = D * VS;                     // bytes of an LDS row
   static constexpr int OB = D * ES;                     // bytes of a row of q and out
   static constexpr int CPR = OB / 16;                   // chunks of it
-  static constexpr int KT = (ES == 2 && !KEYS) ? 64 : 32;   // keys of a tile
+  static constexpr int KT = (ES == 2 && BLK == kRows) ? 64 : 32;   // keys of a tile
   static constexpr int TILE = KT * RB;                  // bytes of a K or V tile
   static constexpr int NW = KEYS ? 1 : 4;
   static constexpr int ROWS = 32 * NW;                  // query rows of a block
   static constexpr int BUFS = KEYS ? 1 : 2;             // buffers of K and of V
   static constexpr int LDS = 2 * BUFS * TILE;
   // rows: the scores run a tile ahead
-  static constexpr bool kAhead = !KEYS && ES == 2 && D == 256;
+  static constexpr bool kAhead = BLK == kRows && ES == 2 && D == 256;
   // waves of a SIMD asked for, and with them blocks of a CU
   static constexpr int PER_SIMD = KEYS ? (OB <= 128 ? 4 : OB <= 256 ? (kCodes ? 3 : 2) : 1) : (LDS <= 64 * 1024 ? 2 : 1);
   static constexpr int LDS_BLOCKS = 160 * 1024 / LDS;
   static constexpr int PER_CU = LDS_BLOCKS < 4 * PER_SIMD / NW ? LDS_BLOCKS : 4 * PER_SIMD / NW;
 };
 
-template <typename CT, typename T, int D, bool KEYS, int NT = 64 * Shape<CT, T, D, KEYS>::NW,
-          int PER_SIMD = Shape<CT, T, D, KEYS>::PER_SIMD>
+template <typename CT, typename T, int D, Block BLK, int NT = 64 * Shape<CT, T, D, BLK>::NW,
+          int PER_SIMD = Shape<CT, T, D, BLK>::PER_SIMD>
 __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs a) {
-  using S = Shape<CT, T, D, KEYS>;
+  using S = Shape<CT, T, D, BLK>;
+  constexpr bool KEYS = S::KEYS;
   constexpr int ES = S::ES, VS = S::VS, RB = S::RB, OB = S::OB, CPR = S::CPR, KT = S::KT, KB = KT / 32, TILE = S::TILE, NW = S::NW;
   constexpr int V_AT = S::BUFS * TILE;                  // LDS: [K, V][buffer][TILE]
   constexpr int ROWS = S::ROWS, NQ = OB / 32;           // chunk pairs of a row
@@ -869,14 +876,21 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, bool f
 //     rows 25 | 30, of 64 rows 29 | 33, of 128 rows 39 | 39.  At head_dim 256 a wave's rows,
 //     accumulators and a tile exceed its registers: 4 rows 61 | 48, 64 requests 1,134 | 1,085;
 //     there is no keys shape for it.
+// Rows or pairs: where the CUs have about one block each and more would come only of a split,
+// the rows shape (816 rows of four requests of 8 heads over 816 keys: 41 us, pairs 55, 57
+// split in two); else pairs (four requests over 4,096 keys, 32, 64, 96, 128 rows: 15.6, 17.9,
+// 20.5, 23.2 us, the rows shape 17.5, 21.1, 23.9, 26.9).  The plan's cost decides.  Widening
+// 8-bit codes takes registers that a second wave does not leave.
+template <typename CT, typename T, int D>
+constexpr bool kHasPairs = sizeof(CT) == 2 && D == 256;
 template <typename CT, typename T, int D>
 constexpr int kKeysRows = sizeof(T) == 4 ? (D == 256 ? 0 : 64) : sizeof(CT) == 1 ? 16 : 8;
 
-template <typename CT, typename T, int D, bool KEYS>
+template <typename CT, typename T, int D, Block BLK>
 void launch(const PagedAttnArgs& a, hipStream_t s) {
   const int64_t total = (int64_t)a.B * a.nkv * a.n_split * a.n_tiles;
   const int grid = static_cast<int>((total + 7) / 8 * 8);
-  paged_attn_kernel<CT, T, D, KEYS><<<grid, 64 * Shape<CT, T, D, KEYS>::NW, 0, s>>>(a);
+  paged_attn_kernel<CT, T, D, BLK><<<grid, 64 * Shape<CT, T, D, BLK>::NW, 0, s>>>(a);
   if (a.n_split > 1) {
     const int64_t rows = (int64_t)a.B * a.nkv * a.M * a.G;
     if (a.n_split <= 8) paged_join_kernel<T, D, 1><<<static_cast<int>((rows + 3) / 4), 256, 0, s>>>(a, sizeof(CT) == 1);
@@ -887,13 +901,21 @@ void launch(const PagedAttnArgs& a, hipStream_t s) {
 template <typename CT, typename T, int D>
 void launch_shape(const PagedAttnArgs& a, hipStream_t s) {
   if constexpr (kKeysRows<CT, T, D> > 0)
-    if (a.M * a.G <= kKeysRows<CT, T, D>) return launch<CT, T, D, true>(a, s);
-  launch<CT, T, D, false>(a, s);
+    if (a.M * a.G <= kKeysRows<CT, T, D>) return launch<CT, T, D, kKeys>(a, s);
+  if constexpr (kHasPairs<CT, T, D>)
+    if (a.pairs) return launch<CT, T, D, kPairs>(a, s);
+  launch<CT, T, D, kRows>(a, s);
 }
 
-template <typename CT, typename T, int D, bool KEYS>
-void plan(PagedAttnArgs& a) {
-  using S = Shape<CT, T, D, KEYS>;
+// What a launch costs without a window, in us where kRows and kPairs are compared.
+template <typename CT, typename T, int D, Block BLK>
+double plan(PagedAttnArgs& a) {
+  using S = Shape<CT, T, D, BLK>;
+  constexpr bool KEYS = S::KEYS;
+  // us of a tile with every slot of a CU taken, measured; a block of pairs alone on its CU
+  // takes 1.95
+  constexpr double kTile = kHasPairs<CT, T, D> ? (BLK == kPairs ? 2.4 : 2.8)
+                                               : 2.2 * S::KT / 64 * D / 128 * (sizeof(T) == 4 ? 16 : 1);
   a.n_tiles = (a.M * a.G + S::ROWS - 1) / S::ROWS;
   const int64_t base = (int64_t)a.B * a.nkv * a.n_tiles;
   const int64_t slots = 256 * S::PER_CU;
@@ -906,14 +928,19 @@ void plan(PagedAttnArgs& a) {
   //     round in which some blocks have ended, and of ragged requests many have nothing
   //     to do (64 tokens over 600 .. 4,000 keys: 195 us unsplit, 148 with one round of
   //     four splits, 132 .. 139 with 5 to 24; all of 2,300 keys: 120 unsplit, 128 .. 138).
+  //     The parts of a split are written and read at 4.7 TB/s.
+  double least = 1e300;
   auto choose = [&](int steps, int most) {
     int best = 1;
-    double least = 1e300;
+    least = 1e300;
     for (int n = 1; n <= std::min(most, steps); ++n) {
       const int per = (steps + n - 1) / n;
       if ((steps + per - 1) / per != n) continue;       // the last splits would be empty
       const double rounds = static_cast<double>(base) * n / slots;
-      const double cost = (KEYS ? (std::max(1.0, rounds) + 0.5) * (per + 3) : std::ceil(rounds) * (per + 2)) + (n > 1 ? 2 : 0);
+      const double parts = KEYS || n == 1 ? 0.0 : base * n * (S::ROWS * D * 8 / 4.7e6) / kTile;
+      const double alone = BLK == kPairs && base * n <= 256 ? 1.95 / 2.4 : 1.0;
+      const double cost = (KEYS ? (std::max(1.0, rounds) + 0.5) * (per + 3) : std::ceil(rounds) * (per + 2) * alone) +
+                          (n > 1 ? 2 : 0) + parts;
       if (cost < least) {
         least = cost;
         best = n;
@@ -925,6 +952,7 @@ void plan(PagedAttnArgs& a) {
   // the longest range of a block; the workspace is sized without the window
   const int steps = std::max(1, (a.max_kv + S::KT - 1) / S::KT);
   a.n_split = choose(steps, 64);
+  const double us = least * kTile;
   int span = steps;
   if (a.window > 0) {
     const int64_t keys = (int64_t)a.window + (S::ROWS - 1) / a.G + 1;
@@ -932,13 +960,23 @@ void plan(PagedAttnArgs& a) {
     a.n_split = choose(span, a.n_split);
   }
   a.split_keys = (span + a.n_split - 1) / a.n_split * S::KT;
+  return us;
 }
 
 template <typename CT, typename T, int D>
 void plan_shape(PagedAttnArgs& a) {
   if constexpr (kKeysRows<CT, T, D> > 0)
-    if (a.M * a.G <= kKeysRows<CT, T, D>) return plan<CT, T, D, true>(a);
-  plan<CT, T, D, false>(a);
+    if (a.M * a.G <= kKeysRows<CT, T, D>) {
+      plan<CT, T, D, kKeys>(a);
+      return;
+    }
+  const double us = plan<CT, T, D, kRows>(a);
+  if constexpr (kHasPairs<CT, T, D>) {
+    // compared without the window, which the size of the workspace does not know
+    PagedAttnArgs p = a;
+    p.pairs = 1;
+    if (plan<CT, T, D, kPairs>(p) < us) a = p;
+  }
 }
 
 template <typename F>

@@ -169,6 +169,27 @@ def test_masks(kind, rows, causal, window):
     run_attention(f"mask {kind} {rows} {causal} {window}", c, rows, 8, new, kv, causal=causal, window=window)
 
 
+@pytest.mark.parametrize("B,rows,nkv,kv_max,ps,causal,window", [
+    (33, 9, 8, 40, 16, True, 0),        # more blocks than CUs: two of a CU
+    (25, 9, 8, 300, 16, False, 0),      # about a block for every CU, keys not split
+    (25, 9, 8, 300, 64, True, 70),
+    (2, 150, 1, 2500, 16, True, 0),     # few blocks: keys split
+    (2, 150, 1, 2500, 64, True, 900),   # the same behind a window, in the workspace sized without it
+    (1, 300, 1, 300, 4096, False, 0)])
+def test_chunks_of_head_dim_256(B, rows, nkv, kv_max, ps, causal, window):
+    kv = [kv_max - 7 * b for b in range(B)]
+    new = [max(0, min(rows, kv[b]) - b) for b in range(B)]
+    c = Cache(11, "bf16", nkv, 256, ps, [max(0, n) for n in kv])
+    kv = [max(0, n) for n in kv]
+    new = [min(m, n) for m, n in zip(new, kv)]
+    H = nkv * (1 if nkv == 8 else 2)
+    size = px().paged_attention_workspace(c.px, H, rows, kv_max)
+    ws = torch.full((max(16, size),), 0x7f, dtype=torch.uint8, device="cuda")
+    a = run_attention(f"256 {B} {rows}", c, rows, H, new, kv, causal=causal, window=window, max_kv_len=kv_max, workspace=ws)
+    b = run_attention("again", c, rows, H, new, kv, causal=causal, window=window, max_kv_len=kv_max, workspace=ws)
+    assert torch.equal(a, b), "two runs of one call differ"
+
+
 @pytest.mark.parametrize("D", DIMS)
 @pytest.mark.parametrize("rows", [1, 40])
 @pytest.mark.parametrize("kind", ["bf16", "fp8"])
