@@ -16,8 +16,8 @@
 // Three shapes of block:
 //   rows   four waves x 32 query rows that share K/V tiles, the next tile under way in a
 //          second buffer: chunks.  Bound by the matrix cores and what goes on beside them:
-//          4,096 rows of 32 heads over 8,192 keys of 128, causal, take 418 .. 449 us from card
-//          to card (920 .. 987 TFLOP/s; the library's product of 8,192^3 reaches 1,116 there),
+//          4,096 rows of 32 heads over 8,192 keys of 128, causal, take 416 .. 449 us from card
+//          to card (917 .. 990 TFLOP/s; the library's product of 8,192^3 reaches 1,116 there),
 //          the matrix cores busy 49 % of the cycles, the LDS 25 %, with 0.5 % of those in
 //          conflict.  At head_dim 256 a CU has one wave a SIMD, and the scores run a tile
 //          ahead so that products and exponentials overlap inside the wave.
@@ -29,7 +29,7 @@
 //          keys 124 us (4.9 TB/s; a large copy moves 4.8, a read alone 6.5), 131,072 keys in
 //          8 bits 167 us (5.6 TB/s), one request over 817 keys 12 us, of which the two
 //          launches are about seven.
-// Either may split the keys over blocks; a second kernel joins the splits (25 us for 64
+// Each may split the keys over blocks; a second kernel joins the splits (25 us for 64
 // splits of 128 rows with one wave a row, 6.5 with four).
 #include "common.hpp"
 #include "errors.hpp"
