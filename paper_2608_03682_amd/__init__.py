@@ -254,7 +254,8 @@ class PrefixLM:
                       workspace=None, status=None, stream=None) -> None:
         """Append the next tokens of each request to a paged cache of all layers
         (``phyai_prefill_paged``).  embeds: device float32 [batch][rows][d];
-        past_len, new_len (default: rows): host arrays."""
+        past_len, new_len (default: rows): host arrays; workspace: as for
+        ``paged_attention``, for the longest past_len + new_len."""
         import torch
         B, rows = int(embeds.shape[0]), int(embeds.shape[1])
         if embeds.dim() != 3 or embeds.dtype != torch.float32 or B != cache.batch or embeds.shape[2] != self.cfg.d_model:
@@ -273,10 +274,10 @@ class PrefixLM:
             need = paged_attention_workspace(cache, self.cfg.n_q_heads, rows, longest)
             if need:
                 workspace = torch.empty(need, dtype=torch.uint8, device=embeds.device)
+        size = 0 if workspace is None else _bytes_of(workspace, embeds)
         _check(lib().phyai_prefill_paged(
             self._h, _ptr(embeds), cache._ref, past.ctypes.data, new.ctypes.data, rows, int(causal),
-            None if workspace is None else workspace.data_ptr(),
-            0 if workspace is None else workspace.numel() * workspace.element_size(),
+            None if workspace is None else workspace.data_ptr(), size,
             _vector(status, torch.int32, 1, embeds, "status"), _here(embeds)))
 
     def profile_stage(self, stage: str, reps: int, stream=None):
@@ -382,6 +383,13 @@ def _vector(t, dtype, least: int, like, what: str) -> Optional[int]:
     if t.dtype != dtype or t.dim() != 1 or t.device != like.device or t.shape[0] < least or not t.is_contiguous():
         raise ValueError(f"{what}: expected {least} contiguous values of {dtype} on {like.device}")
     return t.data_ptr()
+
+
+def _bytes_of(workspace, like) -> int:
+    """The bytes that a workspace owns: plain memory of the call's device."""
+    if workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {like.device}")
+    return workspace.numel() * workspace.element_size()
 
 
 def _elsewhere(t, stream) -> bool:
@@ -567,9 +575,7 @@ def paged_attention(q, cache: PagedCache, kv_len, *, new_len=None, max_kv_len: O
         if size:
             workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     else:
-        if workspace.device != q.device or not workspace.is_contiguous():
-            raise ValueError(f"workspace: expected a contiguous tensor on {q.device}")
-        size = workspace.numel() * workspace.element_size()
+        size = _bytes_of(workspace, q)
     rc = lib().phyai_paged_attention(
         cache._ref, layer, ctypes.byref(qs), ctypes.byref(os_), _vector(kv_len, torch.int32, B, q, "kv_len"),
         _vector(new_len, torch.int32, B, q, "new_len"), max_kv_len, D ** -0.5 if scale is None else scale, causal,

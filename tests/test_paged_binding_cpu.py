@@ -1,0 +1,53 @@
+"""What the binding of the paged cache checks before the library is called, without a GPU:
+tensors on the host stand in for those of a device, and the handle is NULL, which the
+library refuses, so that a call that passes the checks ends there."""
+import ctypes
+from types import SimpleNamespace
+
+import pytest
+
+import paper_2608_03682_amd as px
+from test_paged_cpu import cache
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    monkeypatch.setattr(px, "_elsewhere", lambda t, stream: False)
+    monkeypatch.setattr(px, "_here", lambda t: 0)
+    monkeypatch.setattr(px, "_ptr", lambda t: None if t is None else t.data_ptr())
+
+
+def prefix_lm(d=64):
+    lm = object.__new__(px.PrefixLM)
+    lm.cfg = SimpleNamespace(d_model=d, n_q_heads=8)
+    lm._h = None
+    return lm
+
+
+def paged(batch=2, tokens=4096 * 64):
+    c = cache(batch=batch, max_pages=tokens // 64, table_stride=tokens // 64)
+    return SimpleNamespace(_c=c, _ref=ctypes.byref(c), batch=batch, capacity=tokens, k=torch.zeros(1))
+
+
+def prefill(lm=None, embeds=None, c=None, past=(100000, 0), **kw):
+    (lm or prefix_lm()).prefill_paged(torch.zeros(2, 4, 64) if embeds is None else embeds, c or paged(), past, **kw)
+
+
+def passes(**kw):
+    """The checks of the binding let the call through to the library, which finds no handle."""
+    with pytest.raises(px.PhyaiError, match="NULL handle"):
+        prefill(**kw)
+
+
+def test_prefill_refuses_a_workspace_that_is_not_plain_memory_of_the_device(on_host):
+    need = px.paged_attention_workspace(paged(), 8, 4, 100004)
+    assert need > 16
+    passes()
+    passes(workspace=torch.zeros(need, dtype=torch.uint8))
+    for bad in (torch.zeros(need, dtype=torch.uint8, device="meta"),           # another device
+                torch.zeros(1, dtype=torch.uint8).expand(need),                # states more bytes than it has
+                torch.zeros(2 * need, dtype=torch.uint8)[::2]):                # its neighbours' bytes between
+        with pytest.raises(ValueError, match="workspace"):
+            prefill(workspace=bad)
