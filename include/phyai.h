@@ -470,7 +470,8 @@ int phyai_paged_append(const phyai_paged_cache* cache, int32_t layer, const phya
  * A request with a length out of range gets NaN rows (PHYAI_PAGED_BAD_LENGTH;
  * new_len below 0: none, above rows: `rows` of them).  A page number out of range among those that a row
  * may see makes it, and may make other rows of its request, NaN
- * (PHYAI_PAGED_BAD_PAGE).  Products of BF16 rows are accumulated in 32 bits;
+ * (PHYAI_PAGED_BAD_PAGE).  Pages that lie before the window of every row may have been
+ * given back: their numbers are not judged.  Products of BF16 rows are accumulated in 32 bits;
  * the probabilities enter the second product rounded to BF16. */
 int phyai_paged_attention(const phyai_paged_cache* cache, int32_t layer, const phyai_head_rows* q,
                           const phyai_head_rows* out, const int32_t* kv_len, const int32_t* new_len,

@@ -264,6 +264,10 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   const char* kpool = a.pool.k + kvh * a.pool.head_bytes;
   const char* vpool = a.pool.v + kvh * a.pool.head_bytes;
   const int last_page = (kend - 1) >> a.pool.page_shift;
+  // The first page that a row of the block sees.  The first tile may begin before it: the
+  // program may have given those pages back, so their numbers are not judged, and where
+  // there is none, page 0 is read in its place (no row sees what it holds).
+  const int first_page = seen_begin(tok0, n, kv, a.window) >> a.pool.page_shift;
   // 64 entries of the table from `pbase` on, one per lane; the numbers are checked here
   int pbase = 0, pages = 0;
   auto load_pages = [&](int from) {
@@ -272,7 +276,7 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     int id = 0;
     if (i <= last_page && i < a.pool.max_pages) id = table[i];
     const bool out = !page_ok(id, a.pool.n_pages);
-    if (__ballot(out)) {
+    if (__ballot(out && i >= first_page)) {
       bad = true;
       if (a.status && lane == 0) atomicOr(a.status, PAGED_BAD_PAGE);
     }
