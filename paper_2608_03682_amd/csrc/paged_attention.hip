@@ -679,7 +679,8 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
   // A hidden key's weight is 0, and 0 times an infinite or NaN value is NaN: where a row
   // came out NaN although its weights are numbers, and a key that it does not see but
   // its block does holds such a value, it is computed once more over the keys that it
-  // sees and no other, with the maximum m and sum l found above.
+  // sees and no other, with the maximum m and sum l found above.  The last key stands
+  // again, hidden, behind the end of a last tile that is not full.
   float nan = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
@@ -702,8 +703,9 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
     };
     const int first = max(kbeg, seen_begin(t, n, kv, a.window)), end = min(kend, seen_end(t, n, kv, a.causal));
     bool hidden = false;                                // at most a tile and the block's rows on either side
+    const int behind = (kend - kbeg) % KT ? min(end, kend - 1) : end;
     for (int key = kbeg; key < kend; ++key) {
-      if (key == first && first < end) key = end;
+      if (key == first && first < end) key = behind;
       if (key >= kend) break;
       const int64_t at = row_at(key);
 #pragma unroll

@@ -101,3 +101,38 @@ def test_what_lies_before_the_window_may_be_anything(kind, rows):
     c.table[0, :first] = -1
     check("not named", host(f()), ref, bar)
     check("before", want, ref, bar)
+
+
+# (kind, head_dim, rows, K/V heads, heads of each, keys, split)
+LAST = [("bf16", 64, 3, 1, 2, 61, False), ("bf16", 256, 1, 1, 8, 45, False), ("f32", 128, 2, 1, 4, 45, False),
+        ("bf16", 128, 3, 1, 2, 701, True), ("f32", 64, 3, 1, 2, 701, True), ("bf16", 256, 3, 1, 2, 701, True),
+        ("bf16", 64, 50, 1, 2, 145, False), ("f32", 64, 50, 1, 2, 61, False), ("f32", 256, 2, 1, 4, 61, False),
+        ("bf16", 128, 50, 1, 2, 701, True), ("f32", 128, 50, 1, 2, 701, True), ("bf16", 256, 50, 1, 2, 701, True)]
+
+
+@pytest.mark.parametrize("kind,D,rows,nkv,G,kv,split", LAST)
+def test_an_infinite_value_of_the_last_token(kind, D, rows, nkv, G, kv, split):
+    """The newest token, which ends inside a tile, has an infinite value in one dimension, minus
+    infinity in another and NaN in a third: rows that see it have them, and the others none."""
+    c = shared_cache(24, kind, nkv, D, 16, kv, 1)
+    q = queries(c, 1, rows, nkv * G)
+    assert (px().paged_attention_workspace(c.px, nkv * G, rows, kv) > 0) == split
+    page, at = c.host_table[0, (kv - 1) // 16], (kv - 1) % 16
+    for causal in (True, False):
+        f = lambda: px().paged_attention(q, c.px, ints([kv]), max_kv_len=kv, causal=causal)  # noqa: E731
+        c.v[page, at, 0, [5, 9, 11]] = 0.0
+        want = f()
+        c.v[page, at, 0, 5], c.v[page, at, 0, 9], c.v[page, at, 0, 11] = float("inf"), float("-inf"), float("nan")
+        k, v = c.values()
+        ref, mag = op.paged_attention(host(q), k, np.where(np.isfinite(v), v, 0), c.host_table, [kv], [rows],
+                                      np.zeros(q.shape), causal=causal)
+        bar = attention_bar(kind, host(q), k, ref, mag, D ** -0.5, kv)
+        check("finite", host(want), ref, bar)
+        got = f()
+        see = [rows - 1] if causal else list(range(rows))
+        hide = [t for t in range(rows) if t not in see]
+        rest = [d for d in range(D) if d not in (5, 9, 11)]
+        assert torch.isposinf(got[0, see, :, 5]).all() and torch.isneginf(got[0, see, :, 9]).all()
+        assert got[0, see, :, 11].isnan().all()
+        check("other dimensions", host(got)[..., rest], ref[..., rest], bar[..., rest])
+        check("other rows", host(got)[:, hide], ref[:, hide], bar[:, hide])
