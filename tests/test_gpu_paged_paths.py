@@ -136,3 +136,164 @@ def test_an_infinite_value_of_the_last_token(kind, D, rows, nkv, G, kv, split):
         assert got[0, see, :, 11].isnan().all()
         check("other dimensions", host(got)[..., rest], ref[..., rest], bar[..., rest])
         check("other rows", host(got)[:, hide], ref[:, hide], bar[:, hide])
+
+
+def reference(c, q, kvs, causal=True, window=0):
+    """(o, a, hit): attention over every request's keys in float64 with values that are not finite
+    taken as 0, sum_j p_j |v_j|, and the rows that see a token holding such a value."""
+    k, v = c.values()
+    x = host(q)
+    B, M, H, D = x.shape
+    G = H // k.shape[2]
+    o, mag, hit = np.zeros(x.shape), np.zeros(x.shape), np.zeros((B, M), dtype=bool)
+    for b in range(B):
+        n = kvs[b]
+        if n == 0:
+            continue
+        kb, vb = op.tokens_of(k, c.host_table[b], n), op.tokens_of(v, c.host_table[b], n)
+        odd = ~(np.isfinite(kb).all((1, 2)) & np.isfinite(vb).all((1, 2)))
+        kb, vb = np.where(np.isfinite(kb), kb, 0.0), np.where(np.isfinite(vb), vb, 0.0)
+        ok = op.visible(M, n, causal, window)
+        hit[b] = (ok & odd).any(1)
+        for h in range(H):
+            s = np.where(ok, D ** -0.5 * (x[b, :, h] @ kb[:, h // G].T), -np.inf)
+            p = np.exp(s - np.maximum(s.max(1, keepdims=True), -1e300))
+            p /= np.maximum(p.sum(1, keepdims=True), 1e-300)
+            o[b, :, h], mag[b, :, h] = p @ vb[:, h // G], p @ np.abs(vb[:, h // G])
+    return o, mag, hit
+
+
+def put(c, token, x, heads=slice(None), dims=slice(3, None), pools=("k", "v")):
+    """Value x in a token of the first request."""
+    page, at = c.host_table[0, token // c.ps], token % c.ps
+    for name in pools:
+        pool = getattr(c, name)
+        y = pool[page, at].float()
+        y[heads, dims] = x
+        z = y.to(pool.dtype)
+        pool[page, at].view(torch.uint8 if c.kind == "fp8" else z.dtype).copy_(z.view(torch.uint8) if c.kind == "fp8" else z)
+
+
+# (kind, head_dim, requests, rows, K/V heads, heads of each, keys, window, split)
+PATHS = {
+    # few rows: one wave a block (32 bits at head_dim 256 has the next shape)
+    "few": [("bf16", 64, 1, 3, 1, 2, 61, 20, False), ("bf16", 128, 1, 3, 1, 2, 61, 20, False), ("bf16", 256, 1, 3, 1, 2, 61, 20, False),
+            ("fp8", 64, 1, 3, 1, 2, 61, 20, False), ("fp8", 128, 2, 3, 2, 4, 61, 20, False), ("fp8", 256, 1, 1, 1, 8, 61, 10, False),
+            ("f32", 64, 1, 3, 1, 2, 61, 20, False), ("f32", 128, 1, 3, 1, 2, 61, 20, False)],
+    "few, many requests": [("bf16", 64, 512, 1, 8, 1, 97, 20, False), ("bf16", 128, 256, 1, 8, 1, 97, 20, False),
+                           ("bf16", 256, 128, 1, 8, 1, 97, 20, False), ("fp8", 128, 256, 1, 8, 1, 97, 20, False),
+                           ("f32", 128, 256, 1, 8, 1, 97, 20, False)],
+    "few, split": [("bf16", 64, 1, 3, 1, 2, 2500, 1000, True), ("bf16", 128, 2, 3, 1, 2, 701, 0, True),
+                   ("bf16", 256, 1, 3, 1, 2, 2500, 1000, True), ("fp8", 64, 1, 3, 1, 2, 701, 0, True),
+                   ("fp8", 128, 1, 3, 2, 4, 2500, 1000, True), ("fp8", 256, 1, 3, 1, 2, 2500, 1000, True),
+                   ("f32", 64, 1, 3, 1, 2, 701, 0, True), ("f32", 128, 1, 3, 1, 2, 2500, 1000, True)],
+    "chunk": [("bf16", 64, 1, 50, 1, 2, 150, 40, False), ("bf16", 128, 2, 50, 1, 3, 150, 40, False),
+              ("bf16", 256, 25, 9, 8, 1, 300, 70, False), ("fp8", 64, 1, 50, 1, 2, 150, 40, False),
+              ("fp8", 128, 1, 50, 2, 4, 150, 40, False), ("fp8", 256, 1, 50, 1, 2, 150, 40, False),
+              ("f32", 64, 1, 50, 1, 2, 61, 10, False), ("f32", 128, 1, 50, 1, 2, 61, 10, False), ("f32", 256, 1, 3, 1, 2, 61, 20, False)],
+    "chunk, split": [("bf16", 64, 1, 50, 1, 2, 2500, 990, True), ("bf16", 128, 2, 50, 1, 3, 701, 0, True),
+                     ("bf16", 256, 1, 300, 1, 8, 2500, 0, True), ("fp8", 64, 1, 50, 1, 2, 701, 0, True),
+                     ("fp8", 128, 1, 50, 2, 4, 2500, 990, True), ("fp8", 256, 1, 50, 1, 2, 2500, 990, True),
+                     ("f32", 64, 1, 50, 1, 2, 701, 0, True), ("f32", 128, 1, 50, 1, 2, 2500, 990, True),
+                     ("f32", 256, 1, 50, 1, 2, 2500, 990, True)],
+    # bf16 chunks of head_dim 256 in blocks of which a CU holds two
+    "pairs": [("bf16", 256, 64, 9, 8, 1, 300, 70, False), ("bf16", 256, 33, 9, 8, 1, 61, 0, False)],
+    "pairs, split": [("bf16", 256, 2, 150, 1, 2, 2500, 890, True), ("bf16", 256, 1, 50, 1, 2, 701, 0, True)],
+}
+ALL = [pytest.param(*p, id="-".join([name.replace(", ", "_").replace(" ", "_"), p[0]] + [str(x) for x in p[1:8]]))
+       for name, ps in PATHS.items() for p in ps]
+NAMES = "kind,D,B,rows,nkv,G,kv,window,split"
+
+
+def set_up(seed, kind, D, B, rows, nkv, G, kv, split, ps=16):
+    c = shared_cache(seed, kind, nkv, D, ps, kv, B)
+    assert (px().paged_attention_workspace(c.px, nkv * G, rows, kv) > 0) == split, "another plan than the test means"
+    return c, queries(c, B, rows, nkv * G)
+
+
+@pytest.mark.parametrize(NAMES, ALL)
+def test_lengths_at_the_edges_of_tiles(kind, D, B, rows, nkv, G, kv, window, split):
+    """Every length near a multiple of 32 and of 64, one and none, causal and not, behind a
+    window; the longest keeps the plan.  Two runs give the same bits."""
+    c, q = set_up(31, kind, D, B, rows, nkv, G, kv, split)
+    near = sorted({n for m in range(0, kv + 1, 32) for n in (m - 1, m, m + 1) if 0 <= n <= kv})
+    near = near if len(near) <= 12 else near[:7] + near[-5:]
+    for start in range(0, len(near), B):
+        kvs = [near[(start + b) % len(near)] for b in range(B)]
+        for causal, w in ((True, 0), (False, 0), (True, window)):
+            f = lambda: px().paged_attention(q, c.px, ints(kvs), max_kv_len=kv, causal=causal, window=w)  # noqa: E731
+            got = f()
+            ref, mag, _ = reference(c, q, kvs, causal, w)
+            k, _ = c.values()
+            check(f"{kvs[:4]} causal {causal} window {w}", host(got), ref, attention_bar(kind, host(q), k, ref, mag, D ** -0.5, kv))
+            assert torch.equal(got, f()), "two runs of one call differ"
+
+
+@pytest.mark.parametrize(NAMES, ALL)
+def test_hidden_nan_and_infinities_reach_no_row(kind, D, B, rows, nkv, G, kv, window, split):
+    """NaN and infinities in the newest token, in one of the chunk and just before the window
+    (in a tile that is read): rows that see none of them are what the formula gives without
+    them, rows that do are not finite."""
+    c, q = set_up(32, kind, D, B, rows, nkv, G, kv, split)
+    odd = float("nan") if kind == "fp8" else float("inf")
+    if rows > 1:
+        put(c, kv - 1, odd)
+        put(c, kv - rows + 2, float("nan"))
+    if window:
+        lo = kv - rows + 1 - window
+        assert (lo - 1) // 32 == lo // 32, "the token before the window lies in another tile"
+        put(c, lo - 1, odd, pools=("v",))
+    kvs = [kv] * B
+    got = host(px().paged_attention(q, c.px, ints(kvs), max_kv_len=kv, window=window))
+    ref, mag, hit = reference(c, q, kvs, True, window)
+    assert not hit.all() and (rows == 1 or hit.any())
+    k, _ = c.values()
+    bar = attention_bar(kind, host(q), np.where(np.isfinite(k), k, 0), ref, mag, D ** -0.5, kv)
+    check("rows that see none", got[~hit], ref[~hit], bar[~hit])
+    assert not np.isfinite(got[hit]).all(-1).any()
+
+
+@pytest.mark.parametrize(NAMES, ALL)
+def test_what_rows_see_stays_what_it_is(kind, D, B, rows, nkv, G, kv, window, split):
+    """An infinite value (8 bits: NaN alone, they have no infinity) and a NaN in the first token,
+    which every row sees: those dimensions are infinite and NaN, the others what they were."""
+    c, q = set_up(33, kind, D, B, rows, nkv, G, kv, split)
+    put(c, 0, 0.0, dims=[5, 9], pools=("v",))
+    f = lambda: px().paged_attention(q, c.px, ints([kv] * B), max_kv_len=kv)  # noqa: E731
+    want = f()
+    put(c, 0, float("nan"), dims=9, pools=("v",))
+    if kind != "fp8":
+        put(c, 0, float("inf"), dims=5, pools=("v",))
+    got = f()
+    assert got[..., 9].isnan().all()
+    if kind != "fp8":
+        assert torch.isposinf(got[..., 5]).all()
+    rest = [d for d in range(D) if d not in (5, 9)]
+    assert torch.equal(got[..., rest], want[..., rest])
+
+
+@pytest.mark.parametrize(NAMES, ALL)
+def test_bad_pages_and_lengths(kind, D, B, rows, nkv, G, kv, window, split):
+    """A page or a length out of range: that request becomes NaN and raises the bit, the
+    others keep their bits."""
+    c, q = set_up(34, kind, D, B, rows, nkv, G, kv, split)
+    bad = B - 1
+
+    def call(kvs, new=None):
+        status = ints([0])
+        out = px().paged_attention(q, c.px, ints(kvs), new_len=None if new is None else ints(new), max_kv_len=kv, causal=False,
+                                   status=status)
+        return out, status.item()
+
+    want, status = call([kv] * B)
+    assert status == 0 and torch.isfinite(want).all()
+    last = (kv - 1) // c.ps
+    for at, page in ((0, -1), (last, c.n_pages), (last // 2, -2 ** 31)):
+        c.table.copy_(torch.from_numpy(c.host_table))
+        c.table[bad, at] = page
+        got, status = call([kv] * B)
+        assert status == px().PAGED_BAD_PAGE and got[bad].isnan().all() and torch.equal(got[:bad], want[:bad])
+    c.table.copy_(torch.from_numpy(c.host_table))
+    for n, new in ((kv + 1, None), (-1, None), (kv, rows + 1)):
+        got, status = call([kv] * bad + [n], None if new is None else [rows] * bad + [new])
+        assert status == px().PAGED_BAD_LENGTH and got[bad].isnan().all() and torch.equal(got[:bad], want[:bad])
