@@ -361,11 +361,20 @@ def _dtype_of(t) -> int:
     return d
 
 
+def _in_32_bits(*values):
+    """Refuses what a 32-bit argument of the library cannot hold (ctypes drops the upper bits)."""
+    for x in values:
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{x} is out of range of 32 bits")
+
+
 def _head_rows(t, what: str, like=None) -> _HeadRows:
     """[batch][rows][heads][head_dim] with any strides of the first three dimensions."""
     n, s = t.shape, t.stride()
     if len(n) != 4 or not t.is_cuda:
         raise ValueError(f"{what}: expected a device tensor [batch][rows][heads][head_dim]")
+    if (n[0] | n[1] | n[2] | n[3]) >> 31:
+        _in_32_bits(*n)
     if s[3] != 1:
         raise ValueError(f"{what}: a head's values must be contiguous")
     if like is not None:
@@ -449,6 +458,7 @@ class PagedCache:
         dtype, n, s = _dtype_of(k), k.shape[-4:], k.stride()[-4:]
         if (dtype == 2) != (k_scale is not None) or (dtype == 2) != (v_scale is not None):
             raise ValueError("an 8-bit cache has k_scale and v_scale, another has none")
+        _in_32_bits(*k.shape, *page_table.shape, page_table.stride(0))
         self.k, self.v, self.page_table, self.k_scale, self.v_scale = k, v, page_table, k_scale, v_scale
         self.n_layers = k.shape[0] if k.dim() == 5 else 1
         self.batch, self.page_size, self.n_kv_heads, self.head_dim = page_table.shape[0], n[1], n[2], n[3]
@@ -524,6 +534,8 @@ def paged_append(cache: PagedCache, k, v, past_len, *, new_len=None, rope_base: 
     B, M, _, D = k.shape
     if B != cache.batch or D != cache.head_dim or k.device != cache.k.device:
         raise ValueError("k: batch, head_dim and device must be the cache's")
+    if layer >> 31:
+        _in_32_bits(layer)
     if B * M == 0:
         return
     rc = lib().phyai_paged_append(cache._ref, layer, ctypes.byref(ks), ctypes.byref(vs), rope_base,
@@ -536,8 +548,11 @@ def paged_append(cache: PagedCache, k, v, past_len, *, new_len=None, rope_base: 
 
 def paged_attention_workspace(cache: PagedCache, n_q_heads: int, rows: int, max_kv_len: Optional[int] = None) -> int:
     """Bytes of workspace that such a ``paged_attention`` call needs."""
-    n = lib().phyai_paged_attention_workspace(cache._ref, n_q_heads, rows,
-                                              cache.capacity if max_kv_len is None else max_kv_len)
+    if max_kv_len is None:
+        max_kv_len = cache.capacity
+    if (n_q_heads | rows | max_kv_len) >> 31:
+        _in_32_bits(n_q_heads, rows, max_kv_len)
+    n = lib().phyai_paged_attention_workspace(cache._ref, n_q_heads, rows, max_kv_len)
     if n < 0:
         _check(int(n))
     return n
@@ -570,6 +585,8 @@ def paged_attention(q, cache: PagedCache, kv_len, *, new_len=None, max_kv_len: O
         return out
     if max_kv_len is None:
         max_kv_len = cache.capacity
+    if (layer | window | max_kv_len) >> 31:
+        _in_32_bits(layer, window, max_kv_len)
     if workspace is None:
         size = paged_attention_workspace(cache, H, M, max_kv_len)
         if size:
@@ -595,6 +612,7 @@ def paged_gather(cache: PagedCache, kv_len, rows: int, *, out=None, status=None,
     if _elsewhere(k, stream):
         with _there(k, stream):
             return paged_gather(cache, kv_len, rows, out=out, status=status)
+    _in_32_bits(rows)
     dt = torch.float32 if k.dtype == torch.float32 else torch.bfloat16
     shape = (cache.n_layers, 2, cache.batch, rows, cache.n_kv_heads * cache.head_dim)
     if out is None:

@@ -39,3 +39,33 @@ def test_prefill_refuses_a_workspace_that_is_not_plain_memory_of_the_device():
     torch.cuda.synchronize()
     assert (room[need:] == 0x5a).all() and (room[:need] != 0x5a).any()
     lm.close()
+
+
+def test_a_number_beyond_32_bits_is_refused_and_not_cut():
+    """Not the layer, window, length or row count that is left of it."""
+    big = 2 ** 32
+    k = torch.zeros(2, 3, 16, 1, 64, dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros(1, 2, dtype=torch.int32, device="cuda")
+    c = px().PagedCache(k, k.clone(), table)
+    q, lens = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    x = torch.ones(1, 1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (dict(layer=big), dict(layer=big + 1), dict(layer=-big), dict(window=big + 5), dict(window=1 - big),
+                dict(max_kv_len=big + 16)):
+        with pytest.raises(ValueError, match="32 bits"):
+            px().paged_attention(q, c, lens, **bad)
+    with pytest.raises(ValueError, match="32 bits"):
+        px().paged_append(c, x, x, lens, layer=big)
+    with pytest.raises(ValueError, match="32 bits"):
+        px().paged_gather(c, lens, big + 4, out=torch.zeros(1, device="cuda"))
+    far = q.expand(1, big + 1, 2, 64)
+    for f in (lambda: px().paged_attention(far, c, lens, out=far), lambda: px().qk_norm_rope(far, q_out=far),
+              lambda: px().paged_append(c, x.expand(1, big + 1, 1, 64), x.expand(1, big + 1, 1, 64), lens),
+              lambda: px().PagedCache(k[0, :1].expand(big + 1, 16, 1, 64), k[0, :1].expand(big + 1, 16, 1, 64), table)):
+        with pytest.raises(ValueError, match="32 bits"):
+            f()
+    torch.cuda.synchronize()
+    assert (k == 0).all()
+    # what the library refuses itself it still does
+    for bad in (dict(layer=2), dict(layer=-1), dict(window=-1), dict(max_kv_len=33)):
+        with pytest.raises(px().PhyaiError):
+            px().paged_attention(q, c, lens, **bad)

@@ -51,3 +51,10 @@ def test_prefill_refuses_a_workspace_that_is_not_plain_memory_of_the_device(on_h
                 torch.zeros(2 * need, dtype=torch.uint8)[::2]):                # its neighbours' bytes between
         with pytest.raises(ValueError, match="workspace"):
             prefill(workspace=bad)
+
+
+@pytest.mark.parametrize("heads,rows,longest", [(8 + 2 ** 32, 4, 64), (8, 4 + 2 ** 32, 64), (8, 4, 64 + 2 ** 32), (8, 4, 64 - 2 ** 32)])
+def test_a_number_beyond_32_bits_is_refused_and_not_cut(heads, rows, longest):
+    px.paged_attention_workspace(paged(), 8, 4, 64)
+    with pytest.raises(ValueError, match="32 bits"):
+        px.paged_attention_workspace(paged(), heads, rows, longest)
