@@ -262,10 +262,8 @@ class PrefixLM:
             raise ValueError("embeds: expected float32 [batch of the cache][rows][d_model]")
         if embeds.device != cache.k.device:
             raise ValueError("embeds: the device must be the cache's")
-        past = np.ascontiguousarray(past_len, dtype=np.int32)
-        new = np.full(B, rows, np.int32) if new_len is None else np.ascontiguousarray(new_len, dtype=np.int32)
-        if past.shape[0] < B or new.shape[0] < B:
-            raise ValueError("past_len or new_len shorter than the batch")
+        past = _host_lengths(past_len, B, "past_len")
+        new = _host_lengths(np.full(B, rows) if new_len is None else new_len, B, "new_len")
         if _elsewhere(embeds, stream):
             with _there(embeds, stream):
                 return self.prefill_paged(embeds, cache, past, new, causal=causal, workspace=workspace, status=status)
@@ -392,6 +390,18 @@ def _vector(t, dtype, least: int, like, what: str) -> Optional[int]:
     if t.dtype != dtype or t.dim() != 1 or t.device != like.device or t.shape[0] < least or not t.is_contiguous():
         raise ValueError(f"{what}: expected {least} contiguous values of {dtype} on {like.device}")
     return t.data_ptr()
+
+
+def _host_lengths(x, batch: int, what: str) -> np.ndarray:
+    """Host lengths of at least `batch` requests as int32, none of them changed by that."""
+    x = np.asarray(x)
+    if x.ndim != 1 or x.shape[0] < batch or x.dtype.kind not in "iuf":
+        raise ValueError(f"{what}: expected {batch} whole numbers")
+    with np.errstate(invalid="ignore"):
+        y = np.ascontiguousarray(x, dtype=np.int32)
+    if not (y == x).all():
+        raise ValueError(f"{what}: expected whole numbers of 32 bits")
+    return y
 
 
 def _bytes_of(workspace, like) -> int:

@@ -4,6 +4,7 @@ library refuses, so that a call that passes the checks ends there."""
 import ctypes
 from types import SimpleNamespace
 
+import numpy as np
 import pytest
 
 import paper_2608_03682_amd as px
@@ -58,3 +59,20 @@ def test_a_number_beyond_32_bits_is_refused_and_not_cut(heads, rows, longest):
     px.paged_attention_workspace(paged(), 8, 4, 64)
     with pytest.raises(ValueError, match="32 bits"):
         px.paged_attention_workspace(paged(), heads, rows, longest)
+
+
+@pytest.mark.parametrize("past,new", [
+    ([2 ** 32 + 3, 0], None), ([0, -2 ** 32], None), ([3, 0], [1 + 2 ** 32, 1]), ([0, 2 ** 63], None), ([0.5, 0], None),
+    ([float("nan"), 0], None), ([0, 0], [1.5, 1]), ([[3, 0], [5, 0]], None), (7, None), ([0], None), ([0, 0], [1]), (["3", "0"], None)])
+def test_lengths_of_a_chunk_are_refused_and_not_cut(on_host, past, new):
+    """past_len and new_len are host values of any integer type, or whole numbers; what 32 bits
+    cannot hold used to wrap to a length within the bounds."""
+    with pytest.raises(ValueError, match="past_len|new_len"):
+        prefill(past=past, new_len=new)
+
+
+@pytest.mark.parametrize("past", [[3, 0], (3, 0), np.array([3, 0, 9], np.int64), np.array([3.0, 0.0]), torch.tensor([3, 0]),
+                                  np.array([3, 0], np.uint8)])
+def test_lengths_of_a_chunk_of_any_host_type(on_host, past):
+    passes(past=past)
+    passes(past=past, new_len=past)
