@@ -225,6 +225,7 @@ class PrefixLM:
     def __init__(self, cfg, weights: Dict[str, object], max_batch: Optional[int] = None, stream=None):
         if cfg.variant != "prefix_lm":
             raise ValueError("PrefixLM needs a prefix_lm config")
+        import torch
         self.cfg = cfg
         c = make_config(cfg, max_batch, 0)
         arr, keep = _tensor_array(weights)
@@ -232,6 +233,7 @@ class PrefixLM:
         _check(lib().phyai_load_expert(ctypes.byref(c), arr, len(weights), _stream(stream), ctypes.byref(h)))
         del keep
         self._h = h
+        self.device = torch.device("cuda", torch.cuda.current_device())   # where the library allocated
 
     def prefill(self, embeds, prefix_len, out=None, stream=None):
         """embeds: device float32 [B][prefix_cap][d]; prefix_len: host array.
@@ -260,8 +262,8 @@ class PrefixLM:
         B, rows = int(embeds.shape[0]), int(embeds.shape[1])
         if embeds.dim() != 3 or embeds.dtype != torch.float32 or B != cache.batch or embeds.shape[2] != self.cfg.d_model:
             raise ValueError("embeds: expected float32 [batch of the cache][rows][d_model]")
-        if embeds.device != cache.k.device:
-            raise ValueError("embeds: the device must be the cache's")
+        if embeds.device != cache.k.device or embeds.device != self.device:
+            raise ValueError("embeds: the device must be the cache's and the handle's")
         past = _host_lengths(past_len, B, "past_len")
         new = _host_lengths(np.full(B, rows) if new_len is None else new_len, B, "new_len")
         if _elsewhere(embeds, stream):

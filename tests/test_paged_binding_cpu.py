@@ -24,6 +24,7 @@ def prefix_lm(d=64):
     lm = object.__new__(px.PrefixLM)
     lm.cfg = SimpleNamespace(d_model=d, n_q_heads=8)
     lm._h = None
+    lm.device = torch.device("cpu")
     return lm
 
 
@@ -76,3 +77,12 @@ def test_lengths_of_a_chunk_are_refused_and_not_cut(on_host, past, new):
 def test_lengths_of_a_chunk_of_any_host_type(on_host, past):
     passes(past=past)
     passes(past=past, new_len=past)
+
+
+def test_prefill_refuses_tensors_of_another_device_than_the_handles(on_host):
+    """The weights and buffers of a handle lie on the device that was current when it was loaded."""
+    lm = prefix_lm()
+    passes(lm=lm)
+    lm.device = torch.device("meta")
+    with pytest.raises(ValueError, match="handle"):
+        prefill(lm=lm)
