@@ -127,9 +127,8 @@ struct phyai_expert {
   bool split_act = false;
   void *n_lo = nullptr, *g_lo = nullptr;
   CallDesc* desc = nullptr;
-  // prefix LM over a paged cache: projected rows [q | k | v] of every head, and the
-  // lengths before and after a chunk (descriptors of which only the lengths are used)
-  void* qkv = nullptr;
+  // prefix LM over a paged cache: the lengths before and after a chunk (descriptors of
+  // which only the lengths are used)
   CallDesc *past_desc = nullptr, *kv_desc = nullptr;
   // timestep tables
   void *tau = nullptr, *c1 = nullptr, *cact = nullptr;
@@ -1016,7 +1015,8 @@ void enqueue_prefill_paged(phyai_expert& e, const float* embeds, const phyai_pag
   const int L = e.L, d = e.d, D = e.D, B = cache->batch, R = B * rows;
   const int heads = e.nq + 2 * e.nkv, dtype = e.f32 ? PHYAI_DTYPE_F32 : PHYAI_DTYPE_BF16;
   const float base = e.c.rope ? e.c.rope_base : 0.f;
-  T *n = static_cast<T*>(e.n), *qkv = static_cast<T*>(e.qkv), *o = static_cast<T*>(e.o), *g = static_cast<T*>(e.g);
+  T *n = static_cast<T*>(e.n), *o = static_cast<T*>(e.o), *g = static_cast<T*>(e.g);
+  T* qkv = g;                                           // read for the last time before the MLP
   const int32_t *new_len = e.desc->prefix_len, *past_len = e.past_desc->prefix_len, *kv_len = e.kv_desc->prefix_len;
   const int64_t ld = (int64_t)heads * D;
   const phyai_head_rows q{qkv, rows * ld, ld, D, e.nq};
@@ -1185,7 +1185,9 @@ void load_prefix_lm(const phyai_tensor* tensors, int32_t n_tensors, hipStream_t 
   e->n = e->mem.alloc(Bm * M * d * ab);
   e->q = e->mem.alloc(Bm * M * e->qd * ab);
   e->o = e->mem.alloc(Bm * M * e->qd * ab);
-  e->g = e->mem.alloc(Bm * M * F * ab);
+  // the MLP's rows; between the QKV projection and the attention of a chunk over a paged
+  // cache the projected rows [q | k | v]
+  e->g = e->mem.alloc(Bm * M * std::max(F, e->qd + 2 * e->kd) * ab);
   // key ranges: keys 0 .. M-1 written by the QKV epilogue, the tail to the
   // next multiple of 64 stays zero (attention reads whole tiles)
   e->ldk = (M + 63) / 64 * 64;
@@ -1215,7 +1217,6 @@ void load_prefix_lm(const phyai_tensor* tensors, int32_t n_tensors, hipStream_t 
         const int sk = gemm_split_k(static_cast<int>(R), w->NPT, w->K);
         if (sk > 1) pend = std::max(pend, (int64_t)sk * R * d);
       }
-  e->qkv = e->mem.alloc(Bm * M * (e->qd + 2 * e->kd) * ab);
   e->past_desc = static_cast<CallDesc*>(e->mem.alloc(sizeof(CallDesc)));
   e->kv_desc = static_cast<CallDesc*>(e->mem.alloc(sizeof(CallDesc)));
   e->part = e->mem.alloc_n<float>(part > 0 ? part : 4);

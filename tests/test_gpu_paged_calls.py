@@ -69,3 +69,26 @@ def test_a_number_beyond_32_bits_is_refused_and_not_cut():
     for bad in (dict(layer=2), dict(layer=-1), dict(window=-1), dict(max_kv_len=33)):
         with pytest.raises(px().PhyaiError):
             px().paged_attention(q, c, lens, **bad)
+
+
+@pytest.mark.parametrize("d_mlp", [512, 256])
+def test_a_handle_holds_no_buffer_for_the_paged_path_alone(d_mlp):
+    """512 requests of 816 rows: what a row has by phyai_prefill (residual stream, norm, queries,
+    attention, MLP, cosines, keys and values), the projected rows of a chunk within the MLP's
+    (384 values, so 128 more than an MLP of 256 has)."""
+    cfg = plm_cfg(batch=512, prefix_cap=816, prefix_max=816, d_mlp=d_mlp)
+    case = wl.make_prefill_case(cfg.replace(batch=1), seed=1)
+    rows, d, qd, D, L = 512 * 816, cfg.d_model, 256, cfg.head_dim, cfg.n_layers
+    assert (cfg.n_q_heads + 2 * cfg.n_kv_heads) * D == 384
+    row = 4 * d + 2 * d + 2 * 2 * qd + 2 * max(d_mlp, 384) + 8 * D // 2
+    cached = L * 2 * 512 * 832 * D * 2
+    px().PrefixLM(cfg.replace(batch=1), case.weights).close()      # the context, the library's code
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    before = torch.cuda.mem_get_info()[0]
+    lm = px().PrefixLM(cfg, case.weights)
+    used = before - torch.cuda.mem_get_info()[0]
+    lm.close()
+    print(f"[memory] {used / 2 ** 20:.0f} MiB, rows and cache {(rows * row + cached) / 2 ** 20:.0f} MiB", flush=True)
+    # weights, lengths and the parts of split products: below 100 MB; the projected rows are 321 MB
+    assert used < rows * row + cached + 100e6
