@@ -130,7 +130,7 @@ struct PagedAttnArgs {
 enum PagedKind { PAGED_F32 = 0, PAGED_BF16 = 1, PAGED_FP8 = 2 };
 
 void norm_rope(const NormRopeArgs& a, int D, int kind, hipStream_t s);
-void paged_append(const PagedAppendArgs& a, int D, int row_kind, int pool_kind, hipStream_t s);
+void paged_append(const PagedAppendArgs& a, int D, int pool_kind, hipStream_t s);
 void paged_gather(const PagedGatherArgs& a, int pool_kind, hipStream_t s);
 // Plans the launch (row tiles, key splits) for a.B, M, nkv, G, max_kv and window and
 // gives the floats of workspace it needs, most without a window; paged_attention

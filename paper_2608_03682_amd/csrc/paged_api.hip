@@ -185,7 +185,7 @@ void enqueue_append(const phyai_paged_cache* cache, int layer, const phyai_head_
   a.status = status;
   a.B = cache->batch;
   a.M = rows;
-  paged_append(a, cache->head_dim, kind, pool_kind(cache), s);
+  paged_append(a, cache->head_dim, pool_kind(cache), s);
   HIPC(hipGetLastError());
 }
 

@@ -594,85 +594,83 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
         wait(false);
       }
     }
-  } else if (!S::kAhead && kbeg < kend) {
-    // two buffers: the next tile is under way while this one is worked on
-    uint32_t buf = 0;
-    load_pages(kbeg >> a.pool.page_shift);
-    issue(false, 0, kbeg);
-    issue(true, 0, kbeg);
-    commit(false, 0);
-    commit(true, 0);
-    lds_barrier();
-    for (int k0 = kbeg;; k0 += KT, buf ^= TILE) {
-      const bool more = k0 + KT < kend;
-      if (more) {
-        cover(k0 + KT, k0 + 2 * KT);
-        issue(false, buf ^ TILE, k0 + KT);
-        issue(true, buf ^ TILE, k0 + KT);
+  } else if constexpr (!S::kAhead) {
+    if (kbeg < kend) {
+      // two buffers: the next tile is under way while this one is worked on
+      uint32_t buf = 0;
+      load_pages(kbeg >> a.pool.page_shift);
+      issue(false, 0, kbeg);
+      issue(true, 0, kbeg);
+      commit(false, 0);
+      commit(true, 0);
+      lds_barrier();
+      for (int k0 = kbeg;; k0 += KT, buf ^= TILE) {
+        const bool more = k0 + KT < kend;
+        if (more) {
+          cover(k0 + KT, k0 + 2 * KT);
+          issue(false, buf ^ TILE, k0 + KT);
+          issue(true, buf ^ TILE, k0 + KT);
+        }
+        f32x16 st[KB];
+        bf16x8 pf[2 * KB];
+        scores(st, buf);
+        if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
+        float half = half_max(st);
+        hide(st, half, k0);
+        rescale(half);
+        weights(st, pf);
+        values(st, pf, buf);
+        if constexpr (ES == 2) mfma_pipeline<2 * KB * (D / 32), 2, 2>();
+        if (!more) break;
+        commit(false, buf ^ TILE);
+        commit(true, buf ^ TILE);
+        lds_barrier();
       }
+    }
+  } else {
+    if (kbeg < kend) {
+      // The scores of tile t + 1 are computed beside the exponentials of tile t, so that
+      // the matrix cores work while the vector units do: K runs a tile ahead of V.
+      // K(t) and V(t) lie in buffer t % 2; step t reads K(t + 1) and V(t) and loads
+      // K(t + 2) and V(t + 1), whose buffers the step before was the last to read.
       f32x16 st[KB];
       bf16x8 pf[2 * KB];
-      scores(st, buf);
-      if constexpr (ES == 2) mfma_pipeline<KB * NQ, 1, 4>();
+      load_pages(kbeg >> a.pool.page_shift);
+      issue(false, 0, kbeg);
+      issue(true, 0, kbeg);
+      commit(false, 0);
+      commit(true, 0);
+      if (kbeg + KT < kend) {
+        issue(false, TILE, kbeg + KT);
+        commit(false, TILE);
+      }
+      lds_barrier();
+      scores(st, 0);
       float half = half_max(st);
-      hide(st, half, k0);
+      hide(st, half, kbeg);
+      lds_barrier();
+      uint32_t buf = 0;
+      int k0 = kbeg;
+      for (; k0 + KT < kend; k0 += KT, buf ^= TILE) {
+        const bool more = k0 + 2 * KT < kend;
+        cover(k0 + KT, k0 + 3 * KT);
+        if (more) issue(false, buf, k0 + 2 * KT);
+        issue(true, buf ^ TILE, k0 + KT);
+        rescale(half);
+        f32x16 next[KB];
+        scores_and_values(next, st, buf);
+        half = half_max(next);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) st[kb] = next[kb];
+        hide(st, half, k0 + KT);
+        if (more) commit(false, buf);
+        commit(true, buf ^ TILE);
+        lds_barrier();
+      }
       rescale(half);
       weights(st, pf);
       values(st, pf, buf);
-      if constexpr (ES == 2) mfma_pipeline<2 * KB * (D / 32), 2, 2>();
-      if (!more) break;
-      commit(false, buf ^ TILE);
-      commit(true, buf ^ TILE);
-      lds_barrier();
     }
-  } else if (S::kAhead && kbeg < kend) {
-    // The scores of tile t + 1 are computed beside the exponentials of tile t, so that
-    // the matrix cores work while the vector units do: K runs a tile ahead of V.
-    // K(t) and V(t) lie in buffer t % 2; step t reads K(t + 1) and V(t) and loads
-    // K(t + 2) and V(t + 1), whose buffers the step before was the last to read.
-    f32x16 st[KB];
-    bf16x8 pf[2 * KB];
-    load_pages(kbeg >> a.pool.page_shift);
-    issue(false, 0, kbeg);
-    issue(true, 0, kbeg);
-    commit(false, 0);
-    commit(true, 0);
-    if (kbeg + KT < kend) {
-      issue(false, TILE, kbeg + KT);
-      commit(false, TILE);
-    }
-    lds_barrier();
-    scores(st, 0);
-    float half = half_max(st);
-    hide(st, half, kbeg);
-    lds_barrier();
-    uint32_t buf = 0;
-    int k0 = kbeg;
-    for (; k0 + KT < kend; k0 += KT, buf ^= TILE) {
-      const bool more = k0 + 2 * KT < kend;
-      cover(k0 + KT, k0 + 3 * KT);
-      if (more) issue(false, buf, k0 + 2 * KT);
-      issue(true, buf ^ TILE, k0 + KT);
-      rescale(half);
-      f32x16 next[KB];
-      if constexpr (ES == 2) {
-        scores_and_values(next, st, buf);
-      } else {
-        scores(next, buf ^ TILE);
-        weights(st, pf);
-        values(st, pf, buf);
-      }
-      half = half_max(next);
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) st[kb] = next[kb];
-      hide(st, half, k0 + KT);
-      if (more) commit(false, buf);
-      commit(true, buf ^ TILE);
-      lds_barrier();
-    }
-    rescale(half);
-    weights(st, pf);
-    values(st, pf, buf);
   }
   l_run = pair_sum(l_run);
 

@@ -75,7 +75,7 @@ __device__ __forceinline__ float2 turn(uint64_t freq, int pos) {
   return make_float2(c, s);
 }
 
-// The (cos, sin) of a block's tokens, TPB of them from token i0 on.
+// The (cos, sin) of a block's tokens, the first of which stands at pos0.
 template <int D>
 __device__ __forceinline__ void fill_angles(float2 (&cs)[kMaxTokens][D / 2], const RopeFreq& freq, int tokens, int pos0) {
   for (int x = threadIdx.x; x < tokens * (D / 2); x += kThreads) {
@@ -304,11 +304,10 @@ void norm_rope(const NormRopeArgs& a_in, int D, int kind, hipStream_t s) {
   });
 }
 
-void paged_append(const PagedAppendArgs& a_in, int D, int row_kind, int pool_kind, hipStream_t s) {
+void paged_append(const PagedAppendArgs& a_in, int D, int pool_kind, hipStream_t s) {
   PagedAppendArgs a = a_in;
   a.tokens_per_block = tokens_per_block(a.B, a.M);
   const int grid = a.B * ((a.M + a.tokens_per_block - 1) / a.tokens_per_block);
-  (void)row_kind;
   by_dim(D, [&](auto d) {
     constexpr int kD = decltype(d)::value;
     if (pool_kind == PAGED_F32) paged_append_kernel<float, float, kD><<<grid, kThreads, 0, s>>>(a);
