@@ -485,8 +485,8 @@ int64_t phyai_paged_attention_workspace(const phyai_paged_cache* cache, int32_t 
 
 /* Copy the first kv_len[b] tokens of every request, all layers, into the contiguous
  * prefix that phyai_denoise reads: out [n_layers][2][batch][rows][n_kv_heads *
- * head_dim], F32 for an F32 cache, else BF16 (8-bit codes times their scale, rounded
- * once).  Rows from kv_len[b] on are zero.  kv_len: device, 0 .. rows.  A request
+ * head_dim], F32 for an F32 cache, else BF16 (8-bit codes times their scale in 32 bits,
+ * rounded to BF16).  Rows from kv_len[b] on are zero.  kv_len: device, 0 .. rows.  A request
  * with a length out of range becomes NaN (PHYAI_PAGED_BAD_LENGTH), as do tokens
  * of a page number out of range (PHYAI_PAGED_BAD_PAGE).  `out`: 16-byte aligned. */
 int phyai_paged_gather(const phyai_paged_cache* cache, const int32_t* kv_len, void* out, int32_t rows,

@@ -17,18 +17,21 @@
 //   rows   four waves x 32 query rows that share K/V tiles, the next tile under way in a
 //          second buffer: chunks.  Bound by the matrix cores and what goes on beside them:
 //          4,096 rows of 32 heads over 8,192 keys of 128, causal, take 416 .. 449 us from card
-//          to card (917 .. 990 TFLOP/s; the library's product of 8,192^3 reaches 1,116 there),
-//          the matrix cores busy 49 % of the cycles, the LDS 25 %, with 0.5 % of those in
-//          conflict.  At head_dim 256 a CU has one wave a SIMD, and the scores run a tile
-//          ahead so that products and exponentials overlap inside the wave.
+//          to card, 477 under a slower trace (864 .. 991 TFLOP/s; the library's product of
+//          8,192^3 reaches 1,398 .. 1,450), the matrix cores busy 49 % of the cycles, the LDS
+//          25 %, with 0.5 % of those in conflict; with keys of 64: 260 us, with 8-bit keys of
+//          128: 454.  At head_dim 256 a CU has one wave a SIMD, and the scores run a tile
+//          ahead so that products and exponentials overlap inside the wave.  In 32 bits 1,024
+//          rows of 16 heads over 2,048 keys of 128 take 150 us (86 TFLOP/s; the library's
+//          32-bit product 154).
 //   pairs  the same of bf16 at head_dim 256 with tiles of 32 keys: registers and LDS of two
 //          blocks a CU, whose waves overlap each other instead.  2,048 rows of 8 heads over
 //          8,192 keys: 155 us, the rows shape 170.
 //   keys   one wave on 32 rows, one tile of K and of V in LDS, many waves a CU: few
 //          rows, which are bound by reading K/V: 64 requests of one token over 600 .. 4,000
-//          keys 124 us (4.9 TB/s; a large copy moves 4.8, a read alone 6.5), 131,072 keys in
-//          8 bits 167 us (5.6 TB/s), one request over 817 keys 12 us, of which the two
-//          launches are about seven.
+//          keys 124 .. 130 us (4.6 to 4.9 TB/s; a large copy moves 5.4, a read alone 6.5),
+//          131,072 keys in 8 bits 167 .. 185 us (5.0 to 5.6 TB/s), one request over 817 keys
+//          12 us, of which the two launches are about seven.
 // Each may split the keys over blocks; a second kernel joins the splits (25 us for 64
 // splits of 128 rows with one wave a row, 6.5 with four).
 #include "common.hpp"
@@ -462,7 +465,11 @@ __global__ __launch_bounds__(NT, PER_SIMD) void paged_attn_kernel(PagedAttnArgs 
       m_run = m_new;
     }
   };
-  // P^T of one tile as the B operand, and its sum into l
+  // P^T of one tile as the B operand, and its sum into l.  The matrix cores take 16-bit
+  // operands here, so beside bf16 values p is rounded to bf16 (half a step, 2^-8 of it); a
+  // second term for the rest would double the products of V.  l sums the p that are not
+  // rounded.  Over hundreds of keys the roundings average out: the output's own rounding is 1.7e-3
+  // of its size, and this adds up to 0.04e-3 (four requests of 816 rows over 816 keys).
   auto weights = [&](f32x16 (&st)[KB], bf16x8 (&pf)[2 * KB]) {
     const float m_use = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every p is 0
     float ps[2 * KB];

@@ -2,8 +2,9 @@
 // position rotation in the same pass, appending to the pages, and the gather back
 // into one contiguous prefix per request.  All are bound by memory: every value is
 // read once and written once, 16 bytes a lane.  Norms of 7,800 tokens of 40 heads of 128:
-// 37 us (4.3 TB/s; a large copy moves 4.8); append of 14,600 tokens of 8 + 8 heads: 24 us (4.9);
-// gather of the 18-layer prefix of eight requests: 44 us (5.2); single tokens 4 to 5 us.
+// 37 us (4.3 TB/s; a large copy moves 5.4), in 32 bits 70 (4.6); append of 14,600 tokens of
+// 8 + 8 heads: 24 us (4.9), in 32 bits 51 (4.7), to 8 bits 28 (3.2); gather of the 18-layer prefix of
+// eight requests: 44 us (5.2); single tokens 4 to 5 us.
 //
 // A head's row of D values is the work of D / 16 lanes: lane c holds values
 // 8 c .. 8 c + 7 and their partners at + D / 2, so that a pair rotates inside a lane
